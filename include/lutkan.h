@@ -382,6 +382,72 @@ int lutkan_error_stats(const float *y, const float *y_ref, int64_t B, int32_t m,
                        float t0, float tK, const float *input_domain, int32_t boundary, lutkan_error_summary *out,
                        void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * 8-bit operators around a layer in a language model's block: the norm in front of it and the dense projections into and
+ * out of its width, for one weight or by expert.  Inference only, as the layers are.
+ *
+ * Codes are 8-bit floating point, e4m3 with NaN and without infinities (largest value 448), a byte each.  A scale (fp32) belongs
+ * to each 128 columns of an activation's row, and to each block of 128 rows x 128 columns of a weight; the last block of an
+ * axis may be shorter.  A code stands for code * scale, with
+ *     scale = max(largest magnitude in the block / 448, 2^-126),    code = value / scale rounded to nearest, ties to even
+ * A block with a NaN or an infinity gets a scale that is not finite, and stands for NaN.
+ * Strides are in elements from one row (matrix) to the next; columns are contiguous; any alignment is served.  Rows of an input
+ * may overlap or repeat (stride 0), those of an output may not.
+ * ---------------------------------------------------------------------------------------------- */
+typedef enum { LUTKAN_F32 = 0, LUTKAN_F16 = 1, LUTKAN_BF16 = 2 } lutkan_type;
+
+#define LUTKAN_FP8_MAX_WIDTH 32768          /* columns of a row that is normalised */
+#define LUTKAN_FP8_MAX_INPUTS 1048576       /* inputs or outputs of a product */
+
+/* The residual's addition, the root-mean-square norm and the conversion to codes, in one pass over x [rows][width]:
+ *     h = x + residual (fp32),   y = h / sqrt(mean(h^2) + eps) * weight,   codes and scales of y
+ * residual_out receives h rounded to the residual's type (it may be the residual itself); codes come from the unrounded h.
+ * residual and residual_out are both null or both given.  weight [width].  Errors: EINVAL, ESHAPE (a stride shorter than a
+ * row), EUNSUPPORTED (width), EHIP. */
+typedef struct {
+  const void *x, *residual, *weight;        /* device; residual nullable */
+  void *residual_out, *codes;               /* device; residual_out [rows][width] of residual_type, codes one byte each */
+  float *scales;                            /* device [rows][ceil(width / 128)] */
+  int64_t x_stride, residual_stride, residual_out_stride, codes_stride, scales_stride;
+  int64_t rows;
+  int32_t width;
+  int32_t x_type, residual_type, weight_type;    /* lutkan_type */
+  float eps;                                /* >= 0 */
+} lutkan_rmsnorm_fp8_args;
+int lutkan_rmsnorm_fp8(const lutkan_rmsnorm_fp8_args *args, void *hip_stream);
+
+/* Weights [matrices][n][k] of a lutkan_type to codes [matrices][n][k] (contiguous) and scales
+ * [matrices][ceil(n / 128)][ceil(k / 128)].  Done once, as a model is loaded. */
+int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t matrices, int32_t n, int32_t k, int64_t stride, int64_t matrix_stride,
+                        void *codes, float *scales, void *hip_stream);
+
+/* y[s][j] = sum over blocks b of x_scales[s][b] * weight_scales[j / 128][b] * (sum over k in b of x[s][k] * weight[j][k]).
+ * A block's products are summed on the matrix cores, the blocks in fp32; y is rounded once, to y_type.  The order of the sum
+ * over blocks depends on the sizes, not on the run: equal calls give equal bits.
+ * lutkan_matmul_fp8 takes one weight; rows == x_rows, and the fields from group_sizes on are not read.
+ * lutkan_grouped_matmul_fp8 takes `groups` weights: rows of y in groups, one after the other, group g the next group_sizes[g]
+ * rows (on the device: negative sizes count as 0, and a group ends with the rows at the latest); rows behind the last group are zeros.
+ * With row_index, row s of y comes from row row_index[s] of x (an index outside [0, x_rows) stands for a row of zeros);
+ * without, from row s, and rows == x_rows.
+ * Errors: EINVAL, ESHAPE (strides, row counts), EUNSUPPORTED (sizes), EHIP. */
+typedef struct {
+  const void *x;                            /* device codes [x_rows][k] */
+  const float *x_scales;                    /* device [x_rows][ceil(k / 128)] */
+  const void *weight;                       /* device codes [groups][n][k] */
+  const float *weight_scales;               /* device [groups][ceil(n / 128)][ceil(k / 128)], contiguous */
+  void *y;                                  /* device [rows][n] of y_type */
+  int64_t x_rows, x_stride, x_scales_stride, weight_stride, weight_matrix_stride, y_stride;
+  int64_t rows;
+  int32_t k, n;
+  int32_t y_type;                           /* lutkan_type */
+  int32_t groups;
+  const void *group_sizes;                  /* device [groups], whole numbers of group_sizes_bytes (4 or 8) */
+  const void *row_index;                    /* device [rows], nullable, of row_index_bytes (4 or 8) */
+  int32_t group_sizes_bytes, row_index_bytes;
+} lutkan_matmul_fp8_args;
+int lutkan_matmul_fp8(const lutkan_matmul_fp8_args *args, void *hip_stream);
+int lutkan_grouped_matmul_fp8(const lutkan_matmul_fp8_args *args, void *hip_stream);
+
 /* Measurement aid, not part of the method: launches one kernel of known work that exercises a single resource, so
  * that a caller who times it (events on hip_stream) learns the rate this machine sustains and can put the layer
  * kernels' roofline terms beside measured peaks as well as published ones.

@@ -13,5 +13,5 @@ from .binding import (  # noqa: F401
     lutkan_forward_locate, lutkan_forward_trace, bspline_forward_edges, bspline_forward_locate,
     lutkan_forward_workspace_bytes, lutkan_last_error, lutkan_last_plan, lutkan_chain_forward, lutkan_model_forward,
     lutkan_model_workspace_bytes, lutkan_probe_launch, lutkan_version, load_library, lutkan_forward_static_scratch,
-    STATIC_SCRATCH_BYTES,
+    STATIC_SCRATCH_BYTES, FP8_BLOCK, lutkan_rmsnorm_fp8, lutkan_quantise_fp8, lutkan_matmul_fp8, lutkan_grouped_matmul_fp8,
 )

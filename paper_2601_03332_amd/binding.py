@@ -67,6 +67,19 @@ class _SplineDevLayer(C.Structure):
                 ("input_ext_knots", C.c_void_p)]
 
 
+class _RmsnormFp8Args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "residual", "weight", "residual_out", "codes", "scales")] + \
+               [(n, C.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "codes_stride", "scales_stride", "rows")] + \
+               [(n, C.c_int32) for n in ("width", "x_type", "residual_type", "weight_type")] + [("eps", C.c_float)]
+
+
+class _MatmulFp8Args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "x_scales", "weight", "weight_scales", "y")] + \
+               [(n, C.c_int64) for n in ("x_rows", "x_stride", "x_scales_stride", "weight_stride", "weight_matrix_stride", "y_stride", "rows")] + \
+               [(n, C.c_int32) for n in ("k", "n", "y_type", "groups")] + [("group_sizes", C.c_void_p), ("row_index", C.c_void_p)] + \
+               [("group_sizes_bytes", C.c_int32), ("row_index_bytes", C.c_int32)]
+
+
 EXPORTS = [
     "lutkan_last_error", "lutkan_last_plan", "lutkan_version", "lutkan_compile", "lutkan_artifact_free", "lutkan_artifact_info",
     "lutkan_artifact_q", "lutkan_artifact_scale", "lutkan_artifact_ymin", "lutkan_artifact_knots",
@@ -79,6 +92,7 @@ EXPORTS = [
     "lutkan_error_stats_workspace_bytes", "lutkan_error_stats", "lutkan_forward_static_scratch",
     "lutkan_forward_or_workspace", "lutkan_model_forward_or_workspace",
     "lutkan_wide_table_bytes", "lutkan_wide_table_build",
+    "lutkan_rmsnorm_fp8", "lutkan_quantise_fp8", "lutkan_matmul_fp8", "lutkan_grouped_matmul_fp8",
 ]
 
 _lib = None
@@ -137,6 +151,10 @@ def load_library():
     lib.lutkan_error_stats_workspace_bytes.argtypes = [i64]
     lib.lutkan_error_stats_workspace_bytes.restype = sz
     lib.lutkan_error_stats.argtypes = [vp, vp, i64, i32, vp, i32, C.c_float, C.c_float, vp, i32, vp, vp, sz, vp]
+    lib.lutkan_rmsnorm_fp8.argtypes = [C.POINTER(_RmsnormFp8Args), vp]
+    lib.lutkan_quantise_fp8.argtypes = [vp, i32, i64, i32, i32, i64, i64, vp, vp, vp]
+    lib.lutkan_matmul_fp8.argtypes = [C.POINTER(_MatmulFp8Args), vp]
+    lib.lutkan_grouped_matmul_fp8.argtypes = [C.POINTER(_MatmulFp8Args), vp]
     _lib = lib
     return lib
 
@@ -733,3 +751,149 @@ def lutkan_error_stats(y, y_ref, x, t0: float, tK: float, boundary: int, input_d
 _ERROR_SUMMARY_COUNTS = ("rows_in", "rows_oob", "nan_in", "nan_oob")
 _ERROR_SUMMARY_REALS = ("sum_abs_in", "sum_abs_oob", "max_abs_in", "max_abs_oob", "mae_in", "mae_oob", "oob_any_frac")
 _ERROR_SUMMARY_WORDS = len(_ERROR_SUMMARY_COUNTS) + len(_ERROR_SUMMARY_REALS)
+
+
+# ---------------------------------------------------------------- 8-bit operators around a layer (see lutkan.h)
+FP8_BLOCK = 128                     # columns (and rows of a weight) that share a scale
+_TYPES = None
+
+
+def _type_of(dtype):
+    """lutkan_type of a torch dtype, None for others."""
+    global _TYPES
+    if _TYPES is None:
+        torch = _torch()
+        _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+    return _TYPES.get(dtype)
+
+
+def _blocks(n):
+    return -(-n // FP8_BLOCK)
+
+
+def _check_matrix(who, what, t, shape, device, dtype=None):
+    """A strided CUDA tensor of this shape (None: any length) with contiguous columns; dtype None: any of the three float types."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or t.dim() != len(shape) or any(n is not None and t.shape[i] != n for i, n in enumerate(shape)):
+        raise LutKanError(f"{who}: {what} must be a tensor of shape [{', '.join('any' if n is None else str(n) for n in shape)}]")
+    if (t.dtype != dtype) if dtype is not None else (_type_of(t.dtype) is None):
+        raise LutKanError(f"{who}: {what} must be of dtype {dtype if dtype is not None else 'float32, float16 or bfloat16'}")
+    if not t.is_cuda or t.layout != torch.strided:
+        raise LutKanError(f"{who}: {what} must be a CUDA tensor")
+    if device is not None and t.device != device:
+        raise LutKanError(f"{who}: {what} is on {t.device}, the others are on {device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise LutKanError(f"{who}: {what} must have contiguous columns")
+
+
+def _row_stride(t):
+    """Elements from one row of a matrix to the next; that of a dimension of one row is arbitrary and not used."""
+    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+
+
+def _check_rows_apart(who, what, t):
+    if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise LutKanError(f"{who}: rows of {what} must not overlap")
+
+
+def lutkan_rmsnorm_fp8(x, weight, residual=None, eps: float = 1e-6, residual_out=None):
+    """Residual addition, root-mean-square norm and conversion to 8-bit floating point in one pass, on the current stream.
+    x [rows, width] and residual [rows, width] float32, float16 or bfloat16, each its own; weight [width].
+    Returns (codes, scales, residual_out): float8_e4m3fn [rows, width], float32 [rows, ceil(width / 128)], and x + residual in the
+    residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself."""
+    who, torch = "lutkan_rmsnorm_fp8", _torch()
+    _check_matrix(who, "x", x, (None, None), None)
+    rows, width = x.shape
+    _check_matrix(who, "weight", weight, (width,), x.device)
+    if residual is not None:
+        _check_matrix(who, "residual", residual, (rows, width), x.device)
+        if residual_out is None:
+            residual_out = torch.empty((rows, width), dtype=residual.dtype, device=x.device)
+        else:
+            _check_matrix(who, "residual_out", residual_out, (rows, width), x.device, residual.dtype)
+            _check_rows_apart(who, "residual_out", residual_out)
+    elif residual_out is not None:
+        raise LutKanError(f"{who}: residual_out without a residual")
+    codes = torch.empty((rows, width), dtype=torch.float8_e4m3fn, device=x.device)
+    scales = torch.empty((rows, _blocks(width)), dtype=torch.float32, device=x.device)
+    a = _RmsnormFp8Args(x.data_ptr(), None, weight.data_ptr(), None, codes.data_ptr(), scales.data_ptr())
+    a.x_stride, a.codes_stride, a.scales_stride, a.rows, a.width = _row_stride(x), width, _blocks(width), rows, width
+    a.x_type, a.weight_type, a.eps = _type_of(x.dtype), _type_of(weight.dtype), eps
+    if residual is not None:
+        a.residual, a.residual_out, a.residual_type = residual.data_ptr(), residual_out.data_ptr(), _type_of(residual.dtype)
+        a.residual_stride, a.residual_out_stride = _row_stride(residual), _row_stride(residual_out)
+    with torch.cuda.device(x.device):
+        _check(load_library().lutkan_rmsnorm_fp8(C.byref(a), _stream(x.device)))
+    return codes, scales, residual_out
+
+
+def lutkan_quantise_fp8(weight):
+    """(codes, scales) of a weight [n, k], or of one weight per expert [experts, n, k], for the products below: float8_e4m3fn of
+    the weight's shape and a float32 scale for each block of 128 x 128."""
+    who, torch = "lutkan_quantise_fp8", _torch()
+    _check_matrix(who, "weight", weight, (None,) * (3 if isinstance(weight, torch.Tensor) and weight.dim() == 3 else 2), None)
+    n, k = weight.shape[-2:]
+    codes = torch.empty(weight.shape, dtype=torch.float8_e4m3fn, device=weight.device)
+    scales = torch.empty((*weight.shape[:-2], _blocks(n), _blocks(k)), dtype=torch.float32, device=weight.device)
+    with torch.cuda.device(weight.device):
+        _check(load_library().lutkan_quantise_fp8(weight.data_ptr(), _type_of(weight.dtype), weight.shape[0] if weight.dim() == 3 else 1, n, k,
+                                                  _row_stride(weight), weight.stride(0) if weight.dim() == 3 else 0, codes.data_ptr(),
+                                                  scales.data_ptr(), _stream(weight.device)))
+    return codes, scales
+
+
+def _matmul_fp8(who, x, x_scales, weight, weight_scales, y, dtype, rows, experts):
+    """The checks and arguments that the two products share; `rows` of y, None: as many as x."""
+    torch = _torch()
+    _check_matrix(who, "x", x, (None, None), None, torch.float8_e4m3fn)
+    k, device = x.shape[1], x.device
+    _check_matrix(who, "x_scales", x_scales, (x.shape[0], _blocks(k)), device, torch.float32)
+    _check_matrix(who, "weight", weight, (None, None, k) if experts else (None, k), device, torch.float8_e4m3fn)
+    n = weight.shape[-2]
+    _check_matrix(who, "weight_scales", weight_scales, (*weight.shape[:-2], _blocks(n), _blocks(k)), device, torch.float32)
+    if not weight_scales.is_contiguous():
+        raise LutKanError(f"{who}: weight_scales must be contiguous")
+    rows = x.shape[0] if rows is None else rows
+    if y is None:
+        if _type_of(dtype) is None:
+            raise LutKanError(f"{who}: dtype must be float32, float16 or bfloat16")
+        y = torch.empty((rows, n), dtype=dtype, device=device)
+    else:
+        _check_matrix(who, "y", y, (rows, n), device)
+        _check_rows_apart(who, "y", y)
+    return y, _MatmulFp8Args(x.data_ptr(), x_scales.data_ptr(), weight.data_ptr(), weight_scales.data_ptr(), y.data_ptr(), x.shape[0], _row_stride(x),
+                             _row_stride(x_scales), _row_stride(weight), weight.stride(0) if experts else 0, _row_stride(y), rows, k, n, _type_of(y.dtype))
+
+
+def lutkan_matmul_fp8(x, x_scales, weight, weight_scales, y=None, dtype=None):
+    """y [rows, n] = x [rows, k] times weight [n, k] transposed, both as codes (float8_e4m3fn) with their scales (of lutkan_rmsnorm_fp8
+    and lutkan_quantise_fp8, or a checkpoint's in that layout), on the current stream.  dtype: of y where none is given (float32, which
+    a layer takes, is the default; float16, bfloat16)."""
+    who, torch = "lutkan_matmul_fp8", _torch()
+    y, a = _matmul_fp8(who, x, x_scales, weight, weight_scales, y, torch.float32 if dtype is None else dtype, None, False)
+    with torch.cuda.device(x.device):
+        _check(load_library().lutkan_matmul_fp8(C.byref(a), _stream(x.device)))
+    return y
+
+
+def lutkan_grouped_matmul_fp8(x, x_scales, weight, weight_scales, group_sizes, rows=None, y=None, dtype=None):
+    """lutkan_matmul_fp8 by expert: weight [experts, n, k], the rows of y in groups, one after the other, group e the next group_sizes[e]
+    rows (int32 or int64 [experts], on the device; nothing waits for it); rows of y behind the last group are zeros.
+    rows: int32 or int64 [rows of y], which row of x each row of y comes from (outside x: a row of zeros); None: its own."""
+    who, torch = "lutkan_grouped_matmul_fp8", _torch()
+    for t, what in ((group_sizes, "group_sizes"), (rows, "rows")):
+        if t is None and what == "rows":
+            continue
+        if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or t.dim() != 1 or not t.is_cuda or not t.is_contiguous():
+            raise LutKanError(f"{who}: {what} must be a contiguous int32 or int64 CUDA tensor of one dimension")
+    y, a = _matmul_fp8(who, x, x_scales, weight, weight_scales, y, torch.float32 if dtype is None else dtype, None if rows is None else rows.numel(), True)
+    if group_sizes.numel() != weight.shape[0]:
+        raise LutKanError(f"{who}: group_sizes must have one element for each of the {weight.shape[0]} weights")
+    if group_sizes.device != x.device or (rows is not None and rows.device != x.device):
+        raise LutKanError(f"{who}: group_sizes and rows must be on {x.device}")
+    a.groups, a.group_sizes, a.group_sizes_bytes = weight.shape[0], group_sizes.data_ptr(), group_sizes.element_size()
+    if rows is not None:
+        a.row_index, a.row_index_bytes = rows.data_ptr(), rows.element_size()
+    with torch.cuda.device(x.device):
+        _check(load_library().lutkan_grouped_matmul_fp8(C.byref(a), _stream(x.device)))
+    return y

@@ -1,0 +1,270 @@
+// Conversion to 8-bit floating point (e4m3) with a scale for each 128 columns of a row, after the residual's addition and the
+// root-mean-square norm, and of a weight with a scale for each block of 128 x 128.
+#include "lutkan_fp8.h"
+
+namespace {
+
+struct NormArgs {
+  const unsigned char *x, *residual, *weight;
+  unsigned char *residual_out, *codes;
+  float *scales;
+  int64_t x_stride, residual_stride, residual_out_stride, codes_stride, scales_stride;   // elements from one row to the next
+  int64_t rows;
+  int32_t width, weight_type;
+  float eps, inverse_width;
+};
+
+constexpr int kNoResidual = -1;
+
+// One row is normalised by `row_waves` waves, 64 * 8 * CH columns each; a work-group holds one row, or (row_waves = 1) four.  Every
+// element is read once, stays in a register as fp32, and leaves as its sum with the residual and as its code: lane l of a row's
+// lanes holds the eight columns 8 (l + lanes c), c < CH, so that 16 neighbouring lanes hold one block of 128.
+template <int X, int R, int CH>
+__global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs a, int row_waves) {
+  __shared__ float s_sum[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = row_waves == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 6) + wave : blockIdx.x;
+  if (row >= a.rows) return;                                     // (whole waves of a work-group without a barrier)
+  const int lanes = row_waves * 64, at = row_waves == 1 ? lane : threadIdx.x;
+  const unsigned char *x = a.x + row * a.x_stride * type_bytes(X);
+  float h[CH][8];
+  {
+    Raw8<X> rx[CH];
+    Raw8<R == kNoResidual ? LUTKAN_BF16 : R> rr[CH];
+    const unsigned char *r = R == kNoResidual ? nullptr : a.residual + row * a.residual_stride * type_bytes(R);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {                               // all loads of the row first
+      const int col = 8 * (at + lanes * c);
+      if (col + 8 <= a.width) {
+        rx[c] = load_raw8<X>(x + (size_t)col * type_bytes(X));
+        if constexpr (R != kNoResidual) rr[c] = load_raw8<R>(r + (size_t)col * type_bytes(R));
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = 8 * (at + lanes * c);
+      if (col + 8 <= a.width) {
+        values8<X>(rx[c], h[c]);
+        if constexpr (R != kNoResidual) {
+          float v[8];
+          values8<R>(rr[c], v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) h[c][e] += v[e];
+        }
+      } else {                                                   // the row ends inside these eight columns, or before them
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          h[c][e] = 0.0f;
+          if (col + e < a.width) {
+            h[c][e] = load_one<X>(x + (size_t)(col + e) * type_bytes(X));
+            if constexpr (R != kNoResidual) h[c][e] += load_one<R>(r + (size_t)(col + e) * type_bytes(R));
+          }
+        }
+      }
+    }
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(h[c][e], h[c][e], sum);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+  if (row_waves > 1) {
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    sum = 0.0f;
+    for (int w = 0; w < row_waves; ++w) sum += s_sum[w];
+  }
+  const float inverse_rms = 1.0f / sqrtf(fmaf(sum, a.inverse_width, a.eps));
+  unsigned char *codes = a.codes + row * a.codes_stride;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = 8 * (at + lanes * c);
+    const bool whole = col + 8 <= a.width;
+    float y[8];
+    if (whole) {
+      if (a.weight_type == LUTKAN_F32) values8<LUTKAN_F32>(load_raw8<LUTKAN_F32>(a.weight + (size_t)col * 4), y);
+      else if (a.weight_type == LUTKAN_F16) values8<LUTKAN_F16>(load_raw8<LUTKAN_F16>(a.weight + (size_t)col * 2), y);
+      else values8<LUTKAN_BF16>(load_raw8<LUTKAN_BF16>(a.weight + (size_t)col * 2), y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        y[e] = 0.0f;
+        if (col + e < a.width) {
+          const unsigned char *w = a.weight + (size_t)(col + e) * type_bytes(a.weight_type);
+          y[e] = a.weight_type == LUTKAN_F32 ? load_one<LUTKAN_F32>(w) : a.weight_type == LUTKAN_F16 ? load_one<LUTKAN_F16>(w) : load_one<LUTKAN_BF16>(w);
+        }
+      }
+    }
+    unsigned largest = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = h[c][e] * inverse_rms * y[e];
+      if (whole || col + e < a.width) largest = max(largest, magnitude(y[e]));      // (0 * an infinite norm beyond the row's end is none of its values)
+    }
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) largest = max(largest, (unsigned)__shfl_xor((int)largest, off));
+    const float scale = block_scale(largest);
+    const u32x2 code = codes8(y, scale);
+    if ((at & 15) == 0 && col < a.width) a.scales[row * a.scales_stride + col / kScaleBlock] = scale;
+    if (whole) {
+      store_any(codes + col, code);
+      if constexpr (R != kNoResidual) store8<R>(a.residual_out + (row * a.residual_out_stride + col) * type_bytes(R), h[c]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < a.width) {
+          codes[col + e] = (unsigned char)(code[e >> 2] >> ((e & 3) * 8));
+          if constexpr (R != kNoResidual) store_one<R>(a.residual_out + (row * a.residual_out_stride + col + e) * type_bytes(R), h[c][e]);
+        }
+    }
+  }
+}
+
+template <int X, int R>
+void launch_norm(const NormArgs &a, int waves, int chunks, unsigned groups, unsigned threads, hipStream_t s) {
+  switch (chunks) {
+    case 1: hipLaunchKernelGGL((lutkan_rmsnorm_fp8_kernel<X, R, 1>), dim3(groups), dim3(threads), 0, s, a, waves); break;
+    case 2: hipLaunchKernelGGL((lutkan_rmsnorm_fp8_kernel<X, R, 2>), dim3(groups), dim3(threads), 0, s, a, waves); break;
+    default: hipLaunchKernelGGL((lutkan_rmsnorm_fp8_kernel<X, R, 4>), dim3(groups), dim3(threads), 0, s, a, waves); break;
+  }
+}
+
+template <int X>
+void launch_norm_of(const NormArgs &a, int residual_type, int waves, int chunks, unsigned groups, unsigned threads, hipStream_t s) {
+  switch (a.residual ? residual_type : kNoResidual) {
+    case LUTKAN_F32: launch_norm<X, LUTKAN_F32>(a, waves, chunks, groups, threads, s); break;
+    case LUTKAN_F16: launch_norm<X, LUTKAN_F16>(a, waves, chunks, groups, threads, s); break;
+    case LUTKAN_BF16: launch_norm<X, LUTKAN_BF16>(a, waves, chunks, groups, threads, s); break;
+    default: launch_norm<X, kNoResidual>(a, waves, chunks, groups, threads, s); break;
+  }
+}
+
+struct QuantiseArgs {
+  const unsigned char *w;
+  unsigned char *codes;
+  float *scales;
+  int64_t w_stride, w_matrix_stride, codes_stride, codes_matrix_stride;
+  int32_t n, k, row_blocks, column_blocks;
+};
+
+// A work-group of 256 threads converts one block: 16 lanes a row of 128 columns, eight rows each thread, all in registers between
+// the one read and the one write.
+template <int X>
+__global__ __launch_bounds__(256) void lutkan_quantise_fp8_kernel(const QuantiseArgs a) {
+  __shared__ unsigned s_largest[4];
+  const int column_block = blockIdx.x % a.column_blocks;
+  const int64_t rest = blockIdx.x / a.column_blocks;
+  const int row_block = (int)(rest % a.row_blocks);
+  const int64_t matrix = rest / a.row_blocks;
+  const int col = column_block * kScaleBlock + 8 * (threadIdx.x & 15), row0 = row_block * kScaleBlock + (threadIdx.x >> 4);
+  const unsigned char *w = a.w + (matrix * a.w_matrix_stride + col) * type_bytes(X);
+  const bool whole = col + 8 <= a.k;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 16 * i;
+    if (whole && row < a.n) {
+      values8<X>(load_raw8<X>(w + (int64_t)row * a.w_stride * type_bytes(X)), v[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = row < a.n && col + e < a.k ? load_one<X>(w + ((int64_t)row * a.w_stride + e) * type_bytes(X)) : 0.0f;
+    }
+  }
+  unsigned largest = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) largest = max(largest, magnitude(v[i][e]));
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) largest = max(largest, (unsigned)__shfl_xor((int)largest, off));
+  if ((threadIdx.x & 63) == 0) s_largest[threadIdx.x >> 6] = largest;
+  __syncthreads();
+  largest = max(max(s_largest[0], s_largest[1]), max(s_largest[2], s_largest[3]));
+  const float scale = block_scale(largest);
+  if (threadIdx.x == 0) a.scales[blockIdx.x] = scale;            // the blocks' order is the scales'
+  unsigned char *codes = a.codes + matrix * a.codes_matrix_stride + col;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 16 * i;
+    if (row >= a.n) continue;
+    const u32x2 code = codes8(v[i], scale);
+    if (whole) {
+      store_any(codes + (int64_t)row * a.codes_stride, code);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < a.k) codes[(int64_t)row * a.codes_stride + e] = (unsigned char)(code[e >> 2] >> ((e & 3) * 8));
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" int lutkan_rmsnorm_fp8(const lutkan_rmsnorm_fp8_args *p, void *hip_stream) {
+  const char *who = "lutkan_rmsnorm_fp8";
+  if (!p) return fail(LUTKAN_EINVAL, "%s: null arguments", who);
+  if (p->rows < 0 || p->width < 1) return fail(LUTKAN_EINVAL, "%s: rows %lld, width %d", who, (long long)p->rows, p->width);
+  if (p->width > LUTKAN_FP8_MAX_WIDTH) return fail(LUTKAN_EUNSUPPORTED, "%s: width %d, at most %d", who, p->width, LUTKAN_FP8_MAX_WIDTH);
+  if (!is_type(p->x_type) || !is_type(p->weight_type) || (p->residual && !is_type(p->residual_type))) return fail(LUTKAN_EINVAL, "%s: bad type", who);
+  if (!(p->eps >= 0.0f)) return fail(LUTKAN_EINVAL, "%s: eps must be >= 0", who);
+  if (p->rows == 0) return LUTKAN_OK;
+  if (!p->x || !p->weight || !p->codes || !p->scales) return fail(LUTKAN_EINVAL, "%s: null x / weight / codes / scales", who);
+  if ((p->residual != nullptr) != (p->residual_out != nullptr)) return fail(LUTKAN_EINVAL, "%s: residual and residual_out come together", who);
+  const int64_t blocks = scale_blocks(p->width);
+  if (p->codes_stride < p->width || p->scales_stride < blocks || (p->residual && p->residual_out_stride < p->width))
+    return fail(LUTKAN_ESHAPE, "%s: a row of the outputs is longer than its stride", who);
+  if (p->x_stride < 0 || (p->residual && p->residual_stride < 0)) return fail(LUTKAN_ESHAPE, "%s: negative stride", who);
+  // Waves to a row: one while the launch fills the GPU with a wave a row and the row fits its registers; else enough for eight
+  // columns a lane, so that a few rows are spread over many lanes.
+  int waves = (p->width + 511) / 512, chunks = 1;
+  if (p->rows >= 2048 && waves <= 4) { chunks = waves; waves = 1; }
+  else if (p->rows >= 1024 && waves <= 16) { chunks = waves > 8 ? 4 : waves > 4 ? 2 : 1; waves = (waves + chunks - 1) / chunks; }
+  while (waves > 16) { chunks *= 2; waves = (p->width + 512 * chunks - 1) / (512 * chunks); }
+  const int64_t groups = waves == 1 ? (p->rows + 3) / 4 : p->rows;
+  if (groups > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
+  NormArgs a;
+  a.x = static_cast<const unsigned char *>(p->x); a.residual = static_cast<const unsigned char *>(p->residual);
+  a.weight = static_cast<const unsigned char *>(p->weight); a.residual_out = static_cast<unsigned char *>(p->residual_out);
+  a.codes = static_cast<unsigned char *>(p->codes); a.scales = p->scales;
+  a.x_stride = p->x_stride; a.residual_stride = p->residual_stride; a.residual_out_stride = p->residual_out_stride;
+  a.codes_stride = p->codes_stride; a.scales_stride = p->scales_stride;
+  a.rows = p->rows; a.width = p->width; a.weight_type = p->weight_type; a.eps = p->eps; a.inverse_width = 1.0f / (float)p->width;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const unsigned threads = waves == 1 ? 256u : (unsigned)waves * 64u;
+  switch (p->x_type) {
+    case LUTKAN_F32: launch_norm_of<LUTKAN_F32>(a, p->residual_type, waves, chunks, (unsigned)groups, threads, s); break;
+    case LUTKAN_F16: launch_norm_of<LUTKAN_F16>(a, p->residual_type, waves, chunks, (unsigned)groups, threads, s); break;
+    default: launch_norm_of<LUTKAN_BF16>(a, p->residual_type, waves, chunks, (unsigned)groups, threads, s); break;
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
+  return LUTKAN_OK;
+}
+
+extern "C" int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t matrices, int32_t n, int32_t k, int64_t stride, int64_t matrix_stride,
+                                   void *codes, float *scales, void *hip_stream) {
+  const char *who = "lutkan_quantise_fp8";
+  if (!is_type(type)) return fail(LUTKAN_EINVAL, "%s: bad type", who);
+  if (matrices < 0 || n < 1 || k < 1) return fail(LUTKAN_EINVAL, "%s: %lld matrices of %d x %d", who, (long long)matrices, n, k);
+  if (matrices == 0) return LUTKAN_OK;
+  if (!weight || !codes || !scales) return fail(LUTKAN_EINVAL, "%s: null weight / codes / scales", who);
+  if (stride < 0 || matrix_stride < 0) return fail(LUTKAN_ESHAPE, "%s: negative stride", who);
+  QuantiseArgs a;
+  a.w = static_cast<const unsigned char *>(weight); a.codes = static_cast<unsigned char *>(codes); a.scales = scales;
+  a.w_stride = stride; a.w_matrix_stride = matrix_stride; a.codes_stride = k; a.codes_matrix_stride = (int64_t)n * k;
+  a.n = n; a.k = k; a.row_blocks = (int32_t)scale_blocks(n); a.column_blocks = (int32_t)scale_blocks(k);
+  const int64_t per_matrix = (int64_t)a.row_blocks * a.column_blocks;
+  if (matrices > 0x7fffffff / per_matrix) return fail(LUTKAN_EUNSUPPORTED, "%s: too many blocks", who);
+  const dim3 groups((unsigned)(matrices * per_matrix));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  switch (type) {
+    case LUTKAN_F32: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_F32>, groups, dim3(256), 0, s, a); break;
+    case LUTKAN_F16: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_F16>, groups, dim3(256), 0, s, a); break;
+    default: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_BF16>, groups, dim3(256), 0, s, a); break;
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
+  return LUTKAN_OK;
+}
