@@ -85,7 +85,7 @@ __device__ __forceinline__ float block_scale(unsigned largest) {
 }
 
 // Eight codes of v / scale, rounded to nearest, ties to even.  The quotient is v * inverse corrected by its own remainder, so that it is
-// rounded once: v * inverse alone put 1 in 3000 codes of a bf16 weight on the wrong side of a tie.  |v| <= 448 scale, so it is at most 448;
+// rounded once: v * inverse alone can fall on the other side of a tie.  |v| <= 448 scale, so it is at most 448;
 // infinities and NaN only come with a scale that is not finite either, and then every code is NaN or stands for it.
 __device__ __forceinline__ float quotient(float v, float scale, float inverse) {
   const float q = v * inverse;

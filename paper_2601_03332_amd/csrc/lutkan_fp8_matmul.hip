@@ -110,8 +110,8 @@ struct RowTile { int64_t first, end; int group; };
 
 // Tile `tile` of the rows, cut at the groups' ends: every group's rows in tiles of `height`, then those behind the last group.  The
 // sizes are the caller's, on the device: negative ones count as none, and a group ends with the rows at the latest.  Each wave for
-// itself, a lane a group, 64 groups at a time.
-__device__ __forceinline__ RowTile grouped_tile(const ProductArgs &a, int64_t tile, int height) {
+// itself, a lane a group, 64 groups at a time.  `first_behind`: the first tile behind the last group.
+__device__ __forceinline__ RowTile grouped_tile(const ProductArgs &a, int64_t tile, int height, int64_t *first_behind = nullptr) {
   const int lane = threadIdx.x & 63;
   int64_t row0 = 0, tile0 = 0;
   for (int base = 0; base < a.groups; base += 64) {
@@ -143,8 +143,23 @@ __device__ __forceinline__ RowTile grouped_tile(const ProductArgs &a, int64_t ti
     row0 = __shfl(end, 63);
     tile0 = __shfl(last_tile, 63);
   }
+  if (first_behind) *first_behind = tile0;
   const int64_t at = row0 + (tile - tile0) * height;
   return {at, min(at + height, a.rows), -1};
+}
+
+// A value that every lane of the wave holds, as one.
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return ((int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+// All tiles of the rows, those behind the last group among them.
+__device__ __forceinline__ int64_t grouped_tiles(const ProductArgs &a, int height) {
+  constexpr int64_t kBeyond = (int64_t)1 << 62;
+  int64_t tiles = 0;
+  const RowTile none = grouped_tile(a, kBeyond / height, height, &tiles);
+  const int64_t rest = a.rows - (none.first - (kBeyond / height - tiles) * height);
+  return tiles + (rest + height - 1) / height;
 }
 
 // The row of x behind row `row` of the outputs; -1: none, a row of zeros.
@@ -250,24 +265,218 @@ void launch_direct(const ProductArgs &a, int64_t row_tiles, int waves, hipStream
   hipLaunchKernelGGL((lutkan_fp8_direct_kernel<MT, NT, EXACT, GROUPED>), grid, dim3(64 * waves), waves > 1 ? (size_t)waves * MT * NT * 64 * sizeof(f32x4) : 0, s, a);
 }
 
+// A tile of 16 MT WM rows x 16 NT WN columns for a work-group of WM x WN waves, each 16 MT rows x 16 NT columns of it.  Both operands'
+// blocks of k go through LDS, in two buffers of 128 bytes a row: while a block is multiplied the next is on its way.  A row's eight
+// 16-byte pieces lie in an order that depends on the row (piece_place), so that the 16 rows that a read of 16 lanes takes lie in
+// different banks.
+//   ASYNC: the pieces go from global memory to LDS without passing through registers: needs 16-byte aligned rows and offsets
+//   that fit 32 bits.  Otherwise, and for a last block that is not whole, through registers.
+__device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+
+template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED, bool ASYNC>
+__global__ __launch_bounds__(64 * WM * WN, 512 / (64 * WM * WN)) void lutkan_fp8_tiled_kernel(const ProductArgs a, unsigned row_tiles) {
+  constexpr int kRows = 16 * MT * WM, kCols = 16 * NT * WN, kWaves = WM * WN, kThreads = 64 * kWaves, kStage = (kRows + kCols) * kScaleBlock;
+  constexpr int kXCopies = kRows / 8 / kWaves, kWCopies = kCols / 8 / kWaves;          // of 8 rows, for each wave
+  static_assert(kXCopies * 8 * kWaves == kRows && kWCopies * 8 * kWaves == kCols && kThreads >= kRows && kScaleBlock % (16 * NT) == 0, "tile");
+  extern __shared__ __align__(16) unsigned char s_tiles[];       // [buffer][rows of x, rows of the weight][128], then [buffer][threads] scales
+  float *s_scales = reinterpret_cast<float *>(s_tiles + 2 * kStage);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN, p = lane >> 4;
+  // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, and in a run eight row tiles share a column
+  // tile before the next, so that what an XCD's work-groups read at a time meets in its L2.
+  const unsigned col_tiles = (a.n + kCols - 1) / kCols;
+  if constexpr (GROUPED) row_tiles = (unsigned)uniform(grouped_tiles(a, kRows));
+  const unsigned tiles = row_tiles * col_tiles;
+  if (blockIdx.x >= tiles) return;
+  const unsigned xcd = blockIdx.x % 8, of_xcd = tiles / 8, more = tiles % 8;
+  const unsigned tile = xcd * of_xcd + min(xcd, more) + blockIdx.x / 8;
+  const unsigned band = tile / (8 * col_tiles), in_band = tile - band * 8 * col_tiles, high = min(8u, row_tiles - band * 8);
+  const unsigned row_tile = band * 8 + in_band % high;
+  const int col0 = (int)(in_band / high) * kCols;
+  RowTile t;
+  if constexpr (GROUPED) {
+    t = grouped_tile(a, row_tile, kRows);
+    t.first = uniform(t.first); t.end = uniform(t.end); t.group = __builtin_amdgcn_readfirstlane(t.group);
+  } else {
+    t.first = (int64_t)row_tile * kRows;
+    t.end = min(t.first + kRows, a.rows);
+    t.group = 0;
+  }
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (t.group >= 0) {
+    const unsigned char *w_tile = a.w + t.group * a.w_matrix_stride + (int64_t)col0 * a.w_stride;
+    const unsigned char *x_tile = GROUPED ? a.x : a.x + t.first * a.x_stride;
+    typedef std::conditional_t<ASYNC, unsigned, int64_t> offset_t;
+    offset_t x_from[kXCopies], w_from[kWCopies];                 // the rows that this lane's pieces come from
+    int piece_at[2];                                             // and the columns: place i of row r, the same for every 16 rows
+#pragma unroll
+    for (int c = 0; c < 2; ++c) piece_at[c] = piece_place(c * 8 + (lane >> 3), lane & 7) * 16;        // (its own inverse)
+    static_assert(kXCopies % 2 == 0 && kWCopies % 2 == 0, "copies in pairs");
+#pragma unroll
+    for (int c = 0; c < kXCopies; ++c) {
+      const int64_t row = min(t.first + (wave * kXCopies + c) * 8 + (lane >> 3), t.end - 1);
+      x_from[c] = (offset_t)((GROUPED ? max(source_row<GROUPED>(a, row), (int64_t)0) : row - t.first) * a.x_stride);
+    }
+#pragma unroll
+    for (int c = 0; c < kWCopies; ++c) w_from[c] = (offset_t)((int64_t)min((wave * kWCopies + c) * 8 + (lane >> 3), a.n - 1 - col0) * a.w_stride);
+    const int64_t scale_row = min(t.first + min(tid, kRows - 1), t.end - 1);
+    const float *xs = a.x_scales + max(source_row<GROUPED>(a, scale_row), (int64_t)0) * a.x_scales_stride;
+    const float *ws = a.w_scales + ((int64_t)t.group * a.n_blocks + min(col0 + wn * 16 * NT, a.n - 1) / kScaleBlock) * a.k_blocks;
+    const int whole = a.k / kScaleBlock;
+    u32x4 held[ASYNC ? 1 : kXCopies + kWCopies];
+    // Block b's pieces are asked for, and put into a buffer: at once where they go straight there, else by put().
+    const auto ask = [&](int b) {
+      if constexpr (ASYNC) {
+        unsigned char *to = s_tiles + (b & 1) * kStage;
+#pragma unroll
+        for (int c = 0; c < kXCopies; ++c) copy16_global_to_lds_at(x_tile + (int64_t)b * kScaleBlock, x_from[c] + piece_at[c & 1], to + (wave * kXCopies + c) * 1024);
+#pragma unroll
+        for (int c = 0; c < kWCopies; ++c)
+          copy16_global_to_lds_at(w_tile + (int64_t)b * kScaleBlock, w_from[c] + piece_at[c & 1], to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024);
+      } else {
+#pragma unroll
+        for (int c = 0; c < kXCopies; ++c) held[c] = load_any<u32x4>(x_tile + x_from[c] + (b * kScaleBlock + piece_at[c & 1]));
+#pragma unroll
+        for (int c = 0; c < kWCopies; ++c) held[kXCopies + c] = load_any<u32x4>(w_tile + w_from[c] + (b * kScaleBlock + piece_at[c & 1]));
+      }
+    };
+    const auto put = [&](int b) {
+      if constexpr (!ASYNC) {
+        unsigned char *to = s_tiles + (b & 1) * kStage + lane * 16;
+#pragma unroll
+        for (int c = 0; c < kXCopies; ++c) *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = held[c];
+#pragma unroll
+        for (int c = 0; c < kWCopies; ++c) *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = held[kXCopies + c];
+      }
+    };
+    // The last block, if it is not whole.
+    const auto put_end = [&]() {
+      unsigned char *to = s_tiles + (whole & 1) * kStage + lane * 16;
+      for (int c = 0; c < kXCopies; ++c)
+        *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = piece_at_end(x_tile + x_from[c], whole * kScaleBlock + piece_at[c & 1], a.k);
+      for (int c = 0; c < kWCopies; ++c)
+        *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = piece_at_end(w_tile + w_from[c], whole * kScaleBlock + piece_at[c & 1], a.k);
+    };
+    const int at_row = lane & 15, low = at_row * kScaleBlock + piece_place(at_row, p) * 16, high_half = at_row * kScaleBlock + piece_place(at_row, p + 4) * 16;
+    // One block: the products in a fixed order, each added two products after it was begun; a row subtile's codes are read while the one
+    // before it is multiplied.
+    const auto multiply = [&](int b, float w_scale) {
+      const unsigned char *xt = s_tiles + (b & 1) * kStage + (wm * 16 * MT) * kScaleBlock;
+      const unsigned char *wt = s_tiles + (b & 1) * kStage + (kRows + wn * 16 * NT) * kScaleBlock;
+      const float *scales = s_scales + (b & 1) * kThreads + wm * 16 * MT + at_row;
+      const auto codes = [&](const unsigned char *rows, int sub) {
+        return fragment(*reinterpret_cast<const u32x4 *>(rows + sub * 16 * kScaleBlock + low), *reinterpret_cast<const u32x4 *>(rows + sub * 16 * kScaleBlock + high_half));
+      };
+      Operand<EXACT> wf[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) wf[n].set(codes(wt, n));
+      i32x8 next = codes(xt, 0);
+      float next_scale = scales[0];
+      Operand<EXACT> xf;
+      f32x4 v[3];
+      float scales_of[2];
+#pragma unroll
+      for (int i = 0; i < MT * NT + 2; ++i) {
+        const int m = i / NT, n = i % NT;
+        if (i < MT * NT) {
+          if (n == 0) {
+            xf.set(next);
+            scales_of[m & 1] = next_scale * w_scale;
+            if (m + 1 < MT) {
+              next = codes(xt, m + 1);
+              next_scale = scales[(m + 1) * 16];
+            }
+          }
+          v[i % 3] = block_product(wf[n], xf);
+        }
+        if (i >= 2) {
+          const int of = i - 2;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[of / NT][of % NT][e] = fmaf(scales_of[(of / NT) & 1], v[of % 3][e], acc[of / NT][of % NT][e]);
+          asm volatile("" : "+v"(acc[of / NT][of % NT]));        // (here, not behind the next branch, with all products held until then)
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    float scale = xs[0], w_scale = ws[0];
+    if (whole > 0) {
+      ask(0);
+      put(0);
+    }
+    s_scales[tid] = scale;                                       // (threads beyond the rows: the last row's again, behind the others)
+    for (int b = 0; b < whole; ++b) {
+      wait_all_vector_loads();
+      lds_barrier();                                             // block b is there, and nobody reads the other buffer any more
+      scale = xs[min(b + 1, a.k_blocks - 1)];                    // (before the copies: a wait for these does not have to wait for them)
+      const float next_w_scale = ws[min(b + 1, a.k_blocks - 1)];
+      if (b + 1 < whole) ask(b + 1);
+      multiply(b, w_scale);
+      w_scale = next_w_scale;
+      if (b + 1 < whole) put(b + 1);
+      s_scales[((b + 1) & 1) * kThreads + tid] = scale;
+    }
+    if (whole < a.k_blocks) {
+      put_end();                                                 // (into the buffer that nobody reads since the last barrier)
+      lds_barrier();
+      multiply(whole, w_scale);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int64_t row = t.first + (wm * MT + m) * 16 + (lane & 15);
+    if (row >= t.end) continue;
+    const bool none = t.group < 0 || source_row<GROUPED>(a, row) < 0;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) store_outputs(a, row, col0 + (wn * NT + n) * 16 + 4 * p, none ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[m][n]);
+  }
+}
+
+template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED>
+hipError_t launch_tiled(const ProductArgs &a, int64_t row_tiles, hipStream_t s) {
+  constexpr int kRows = 16 * MT * WM, kCols = 16 * NT * WN;
+  constexpr int kLds = 2 * (kRows + kCols) * kScaleBlock + 2 * 64 * WM * WN * (int)sizeof(float);
+  const int64_t grid = row_tiles * ((a.n + kCols - 1) / kCols);
+  const int64_t x_span = (GROUPED ? a.x_rows : kRows) * a.x_stride, w_span = kCols * a.w_stride;
+  const bool async = ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 15) == 0 &&
+                     x_span < ((int64_t)1 << 32) && w_span < ((int64_t)1 << 32);
+  const auto go = [&](auto kernel) {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WM * WN), kLds, s, a, (unsigned)row_tiles);
+    return hipSuccess;
+  };
+  lutkan::plan_note("fp8_tiled rows=%d columns=%d%s; ", kRows, kCols, async ? " async" : "");
+  return async ? go(lutkan_fp8_tiled_kernel<MT, NT, WM, WN, EXACT, GROUPED, true>) : go(lutkan_fp8_tiled_kernel<MT, NT, WM, WN, EXACT, GROUPED, false>);
+}
+
 template <bool EXACT, bool GROUPED>
 int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   const int groups = GROUPED ? a.groups : 1;
   const auto tiles = [&](int height) {                           // no routing has more
     return GROUPED ? a.rows / height + std::min<int64_t>(groups + 1, a.rows) : (a.rows + height - 1) / height;
   };
-  const bool few = a.rows <= 32 * (int64_t)groups;
-  const int height = few ? 16 : 64;
-  if (tiles(height) > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
+  if (tiles(64) * ((a.n + 63) / 64) > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   lutkan::plan_clear();
-  if (few) {
+  const int64_t large = tiles(256) * ((a.n + 255) / 256);        // (at least three quarters of the compute units get a tile)
+  int pick = a.rows <= 32 * (int64_t)groups ? 0 : a.rows < 128 * (int64_t)groups ? 1 : EXACT || large < 192 ? 2 : 3;
+  if (pick == 0) {
+    if (tiles(16) > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
     const int waves = std::max(1, std::min(a.k_blocks, 16));
     lutkan::plan_note("fp8_direct rows=16 columns=16 waves=%d; ", waves);
     launch_direct<1, 1, EXACT, GROUPED>(a, tiles(16), waves, s);
-  } else {
+  } else if (pick == 1) {
+    if (tiles(64) > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
     const int waves = std::max(1, std::min(a.k_blocks, 4));
     lutkan::plan_note("fp8_direct rows=64 columns=64 waves=%d; ", waves);
     launch_direct<4, 4, EXACT, GROUPED>(a, tiles(64), waves, s);
+  } else {
+    hipError_t e;
+    if constexpr (EXACT) e = launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), s);
+    else e = pick == 2 ? launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), s) : launch_tiled<8, 4, 2, 4, EXACT, GROUPED>(a, tiles(256), s);
+    if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
