@@ -164,7 +164,7 @@ _native = None
 
 class _GeneralPath:
     """In place of the module where it cannot be loaded: every call takes the general path."""
-    lut_forward = lut_model_forward = spline_forward = staticmethod(lambda layer, x: None)
+    lut_forward = lut_model_forward = spline_forward = rmsnorm_fp8 = quantise_fp8 = matmul_fp8 = staticmethod(lambda *args: None)
 
 
 def _load_native():
@@ -175,7 +175,8 @@ def _load_native():
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         entries = (lib.lutkan_forward_or_workspace, lib.lutkan_forward, lib.lutkan_model_forward_or_workspace, lib.lutkan_model_forward,
-                   lib.bspline_forward_workspace_bytes, lib.bspline_kan_forward)
+                   lib.bspline_forward_workspace_bytes, lib.bspline_kan_forward, lib.lutkan_rmsnorm_fp8, lib.lutkan_quantise_fp8,
+                   lib.lutkan_matmul_fp8, lib.lutkan_grouped_matmul_fp8)
         module.init(*[C.cast(f, C.c_void_p).value for f in entries], _DevLayer, _SplineDevLayer,
                     getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream))
         return module
@@ -801,6 +802,10 @@ def lutkan_rmsnorm_fp8(x, weight, residual=None, eps: float = 1e-6, residual_out
     x [rows, width] and residual [rows, width] float32, float16 or bfloat16, each its own; weight [width].
     Returns (codes, scales, residual_out): float8_e4m3fn [rows, width], float32 [rows, ceil(width / 128)], and x + residual in the
     residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself."""
+    if residual_out is None:
+        out = (_native or _native_calls()).rmsnorm_fp8(x, weight, residual, eps)
+        if out is not None:
+            return out
     who, torch = "lutkan_rmsnorm_fp8", _torch()
     _check_matrix(who, "x", x, (None, None), None)
     rows, width = x.shape
@@ -830,6 +835,9 @@ def lutkan_rmsnorm_fp8(x, weight, residual=None, eps: float = 1e-6, residual_out
 def lutkan_quantise_fp8(weight):
     """(codes, scales) of a weight [n, k], or of one weight per expert [experts, n, k], for the products below: float8_e4m3fn of
     the weight's shape and a float32 scale for each block of 128 x 128."""
+    out = (_native or _native_calls()).quantise_fp8(weight)
+    if out is not None:
+        return out
     who, torch = "lutkan_quantise_fp8", _torch()
     _check_matrix(who, "weight", weight, (None,) * (3 if isinstance(weight, torch.Tensor) and weight.dim() == 3 else 2), None)
     n, k = weight.shape[-2:]
@@ -870,7 +878,12 @@ def lutkan_matmul_fp8(x, x_scales, weight, weight_scales, y=None, dtype=None):
     and lutkan_quantise_fp8, or a checkpoint's in that layout), on the current stream.  dtype: of y where none is given (float32, which
     a layer takes, is the default; float16, bfloat16)."""
     who, torch = "lutkan_matmul_fp8", _torch()
-    y, a = _matmul_fp8(who, x, x_scales, weight, weight_scales, y, torch.float32 if dtype is None else dtype, None, False)
+    dtype = torch.float32 if dtype is None else dtype
+    if y is None:
+        out = (_native or _native_calls()).matmul_fp8(x, x_scales, weight, weight_scales, dtype)
+        if out is not None:
+            return out
+    y, a = _matmul_fp8(who, x, x_scales, weight, weight_scales, y, dtype, None, False)
     with torch.cuda.device(x.device):
         _check(load_library().lutkan_matmul_fp8(C.byref(a), _stream(x.device)))
     return y
@@ -881,12 +894,17 @@ def lutkan_grouped_matmul_fp8(x, x_scales, weight, weight_scales, group_sizes, r
     rows (int32 or int64 [experts], on the device; nothing waits for it); rows of y behind the last group are zeros.
     rows: int32 or int64 [rows of y], which row of x each row of y comes from (outside x: a row of zeros); None: its own."""
     who, torch = "lutkan_grouped_matmul_fp8", _torch()
+    dtype = torch.float32 if dtype is None else dtype
+    if y is None:
+        out = (_native or _native_calls()).matmul_fp8(x, x_scales, weight, weight_scales, dtype, group_sizes, rows)
+        if out is not None:
+            return out
     for t, what in ((group_sizes, "group_sizes"), (rows, "rows")):
         if t is None and what == "rows":
             continue
         if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or t.dim() != 1 or not t.is_cuda or not t.is_contiguous():
             raise LutKanError(f"{who}: {what} must be a contiguous int32 or int64 CUDA tensor of one dimension")
-    y, a = _matmul_fp8(who, x, x_scales, weight, weight_scales, y, torch.float32 if dtype is None else dtype, None if rows is None else rows.numel(), True)
+    y, a = _matmul_fp8(who, x, x_scales, weight, weight_scales, y, dtype, None if rows is None else rows.numel(), True)
     if group_sizes.numel() != weight.shape[0]:
         raise LutKanError(f"{who}: group_sizes must have one element for each of the {weight.shape[0]} weights")
     if group_sizes.device != x.device or (rows is not None and rows.device != x.device):

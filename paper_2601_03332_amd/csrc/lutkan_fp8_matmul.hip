@@ -434,22 +434,24 @@ __global__ __launch_bounds__(64 * WM * WN, 512 / (64 * WM * WN)) void lutkan_fp8
   }
 }
 
-template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED>
-hipError_t launch_tiled(const ProductArgs &a, int64_t row_tiles, hipStream_t s) {
+template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED, bool ASYNC>
+int launch_tiled(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
   constexpr int kRows = 16 * MT * WM, kCols = 16 * NT * WN;
   constexpr int kLds = 2 * (kRows + kCols) * kScaleBlock + 2 * 64 * WM * WN * (int)sizeof(float);
-  const int64_t grid = row_tiles * ((a.n + kCols - 1) / kCols);
-  const int64_t x_span = (GROUPED ? a.x_rows : kRows) * a.x_stride, w_span = kCols * a.w_stride;
+  static LdsCap cap;
+  const auto kernel = lutkan_fp8_tiled_kernel<MT, NT, WM, WN, EXACT, GROUPED, ASYNC>;
+  if (int rc = raise_lds_cap(kernel, &cap, who)) return rc;
+  lutkan::plan_note("fp8_tiled rows=%d columns=%d%s; ", kRows, kCols, ASYNC ? " async" : "");
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * ((a.n + kCols - 1) / kCols))), dim3(64 * WM * WN), kLds, s, a, (unsigned)row_tiles);
+  return check_launch(who);
+}
+
+template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED>
+int launch_tiled(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
+  const int64_t x_span = (GROUPED ? a.x_rows : 16 * MT * WM) * a.x_stride, w_span = 16 * NT * WN * a.w_stride;
   const bool async = ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 15) == 0 &&
                      x_span < ((int64_t)1 << 32) && w_span < ((int64_t)1 << 32);
-  const auto go = [&](auto kernel) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WM * WN), kLds, s, a, (unsigned)row_tiles);
-    return hipSuccess;
-  };
-  lutkan::plan_note("fp8_tiled rows=%d columns=%d%s; ", kRows, kCols, async ? " async" : "");
-  return async ? go(lutkan_fp8_tiled_kernel<MT, NT, WM, WN, EXACT, GROUPED, true>) : go(lutkan_fp8_tiled_kernel<MT, NT, WM, WN, EXACT, GROUPED, false>);
+  return async ? launch_tiled<MT, NT, WM, WN, EXACT, GROUPED, true>(a, row_tiles, who, s) : launch_tiled<MT, NT, WM, WN, EXACT, GROUPED, false>(a, row_tiles, who, s);
 }
 
 template <bool EXACT, bool GROUPED>
@@ -473,14 +475,10 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
     lutkan::plan_note("fp8_direct rows=64 columns=64 waves=%d; ", waves);
     launch_direct<4, 4, EXACT, GROUPED>(a, tiles(64), waves, s);
   } else {
-    hipError_t e;
-    if constexpr (EXACT) e = launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), s);
-    else e = pick == 2 ? launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), s) : launch_tiled<8, 4, 2, 4, EXACT, GROUPED>(a, tiles(256), s);
-    if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
+    if constexpr (EXACT) return launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), who, s);
+    else return pick == 2 ? launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), who, s) : launch_tiled<8, 4, 2, 4, EXACT, GROUPED>(a, tiles(256), who, s);
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
-  return LUTKAN_OK;
+  return check_launch(who);
 }
 
 int check_product(const lutkan_matmul_fp8_args *p, const char *who, ProductArgs *a) {

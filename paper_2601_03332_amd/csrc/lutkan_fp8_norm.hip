@@ -238,9 +238,7 @@ extern "C" int lutkan_rmsnorm_fp8(const lutkan_rmsnorm_fp8_args *p, void *hip_st
     case LUTKAN_F16: launch_norm_of<LUTKAN_F16>(a, p->residual_type, waves, chunks, (unsigned)groups, threads, s); break;
     default: launch_norm_of<LUTKAN_BF16>(a, p->residual_type, waves, chunks, (unsigned)groups, threads, s); break;
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
-  return LUTKAN_OK;
+  return check_launch(who);
 }
 
 extern "C" int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t matrices, int32_t n, int32_t k, int64_t stride, int64_t matrix_stride,
@@ -264,7 +262,5 @@ extern "C" int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t mat
     case LUTKAN_F16: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_F16>, groups, dim3(256), 0, s, a); break;
     default: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_BF16>, groups, dim3(256), 0, s, a); break;
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(LUTKAN_EHIP, "%s: %s", who, hipGetErrorString(e));
-  return LUTKAN_OK;
+  return check_launch(who);
 }
