@@ -105,61 +105,102 @@ __device__ __forceinline__ void store_outputs(const ProductArgs &a, int64_t row,
   for (int e = 0; e < 4; ++e) if (col + e < a.n) store_any(p + 2 * e, (unsigned short)bits[e]);
 }
 
+// A row's outputs of NT neighbouring column subtiles.  16-bit ones: the 16-lane groups of a pair of subtiles change places, so that a
+// lane holds eight neighbouring outputs, 16 bytes, and a store instruction covers 64 bytes of each of its rows instead of 32.
+template <int NT>
+__device__ __forceinline__ void store_row(const ProductArgs &a, int64_t row, bool exists, int col0, int p, const f32x4 (&v)[NT]) {
+  static_assert(NT % 2 == 0, "pairs");
+  if (a.y_type == LUTKAN_F32) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) if (exists) store_outputs(a, row, col0 + 16 * n + 4 * p, v[n]);
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < NT; n += 2) {
+    unsigned bits[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bits[h][e] = a.y_type == LUTKAN_F16 ? f16_bits(v[n + h][e]) : bf16_bits(v[n + h][e]);
+    const u32x2 low = __builtin_amdgcn_permlane16_swap(bits[0][0] | (bits[0][1] << 16), bits[1][0] | (bits[1][1] << 16), false, false);
+    const u32x2 high = __builtin_amdgcn_permlane16_swap(bits[0][2] | (bits[0][3] << 16), bits[1][2] | (bits[1][3] << 16), false, false);
+    const u32x4 eight{low[0], high[0], low[1], high[1]};
+    const int col = col0 + 16 * n + 16 * (p & 1) + 8 * (p >> 1);
+    if (!exists || col >= a.n) continue;
+    unsigned char *to = a.y + (row * a.y_stride + col) * 2;
+    if (col + 8 <= a.n) { store_any(to, eight); continue; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (col + e < a.n) store_any(to + 2 * e, (unsigned short)(eight[e >> 1] >> ((e & 1) * 16)));
+  }
+}
+
 // Rows [first, end) of the tile, of one group; group < 0: rows behind the last group, whose outputs are zeros.  end <= first: none.
 struct RowTile { int64_t first, end; int group; };
 
-// Tile `tile` of the rows, cut at the groups' ends: every group's rows in tiles of `height`, then those behind the last group.  The
-// sizes are the caller's, on the device: negative ones count as none, and a group ends with the rows at the latest.  Each wave for
-// itself, a lane a group, 64 groups at a time.  `first_behind`: the first tile behind the last group.
-__device__ __forceinline__ RowTile grouped_tile(const ProductArgs &a, int64_t tile, int height, int64_t *first_behind = nullptr) {
-  const int lane = threadIdx.x & 63;
-  int64_t row0 = 0, tile0 = 0;
-  for (int base = 0; base < a.groups; base += 64) {
-    int64_t size = 0;
-    if (base + lane < a.groups) size = a.group_sizes_bytes == 8 ? static_cast<const int64_t *>(a.group_sizes)[base + lane] : static_cast<const int32_t *>(a.group_sizes)[base + lane];
-    size = size < 0 ? 0 : size > a.rows ? a.rows : size;
-    int64_t end = size;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int64_t below = __shfl_up(end, off);
-      if (lane >= off) end += below;
+// The sum of v over the lanes up to and with the own one: shifts within rows of 16 lanes, then the rows' ends handed on.
+__device__ __forceinline__ int lanes_below(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);       // lane 15 of a row to the next, in rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);       // lane 31 to rows 2 and 3
+  return v;
+}
+
+// 64 groups, a lane each: the rows of a group and its tiles of HEIGHT rows, counted from the first group on.  The sizes are the caller's,
+// on the device: negative ones count as none, and a group ends with the rows at the latest.  (At most 2^24 rows: sums of 64 sizes
+// stay below 2^31.)
+template <int HEIGHT>
+struct GroupTiles {
+  int first, end, tiles_before, tiles_with;
+  __device__ __forceinline__ GroupTiles(const ProductArgs &a, int base, int row0, int tile0) {
+    const int group = base + (threadIdx.x & 63), rows = (int)a.rows;
+    int size = 0;
+    if (group < a.groups) {
+      if (a.group_sizes_bytes == 8) size = (int)max((int64_t)0, min(static_cast<const int64_t *>(a.group_sizes)[group], a.rows));
+      else size = max(0, min(static_cast<const int32_t *>(a.group_sizes)[group], rows));
     }
-    const int64_t first = min(row0 + end - size, a.rows);
-    end = min(row0 + end, a.rows);
-    const int64_t own = (end - first + height - 1) / height;
-    int64_t last_tile = own;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int64_t below = __shfl_up(last_tile, off);
-      if (lane >= off) last_tile += below;
-    }
-    last_tile += tile0;
-    const unsigned long long here = __ballot(tile < last_tile);
-    if (here != 0) {
-      const int owner = __builtin_amdgcn_readfirstlane(__builtin_ctzll(here));
-      const int64_t at = __shfl(first, owner) + (tile - (__shfl(last_tile, owner) - __shfl(own, owner))) * height;
-      return {at, min(at + height, __shfl(end, owner)), base + owner};
-    }
-    row0 = __shfl(end, 63);
-    tile0 = __shfl(last_tile, 63);
+    const int with = lanes_below(size);
+    first = min(row0 + with - size, rows);
+    end = min(row0 + with, rows);
+    const int own = (end - first + HEIGHT - 1) / HEIGHT;
+    tiles_with = tile0 + lanes_below(own);
+    tiles_before = tiles_with - own;
   }
-  if (first_behind) *first_behind = tile0;
-  const int64_t at = row0 + (tile - tile0) * height;
-  return {at, min(at + height, a.rows), -1};
-}
+};
 
-// A value that every lane of the wave holds, as one.
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  return ((int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
-}
-
-// All tiles of the rows, those behind the last group among them.
-__device__ __forceinline__ int64_t grouped_tiles(const ProductArgs &a, int height) {
-  constexpr int64_t kBeyond = (int64_t)1 << 62;
-  int64_t tiles = 0;
-  const RowTile none = grouped_tile(a, kBeyond / height, height, &tiles);
-  const int64_t rest = a.rows - (none.first - (kBeyond / height - tiles) * height);
-  return tiles + (rest + height - 1) / height;
+// A tile of the rows, cut at the groups' ends: every group's rows in tiles of HEIGHT, then those behind the last group.  Each wave for
+// itself.  tile_of(number of all tiles): which one, negative: none.
+template <int HEIGHT, typename TileOf>
+__device__ __forceinline__ RowTile grouped_tile(const ProductArgs &a, const TileOf &tile_of) {
+  int row = 0, tiles = 0, base = 0;
+  GroupTiles<HEIGHT> g(a, 0, 0, 0);
+  for (;;) {                                                     // all tiles
+    row = __builtin_amdgcn_readlane(g.end, 63);
+    tiles = __builtin_amdgcn_readlane(g.tiles_with, 63);
+    if (base + 64 >= a.groups) break;
+    base += 64;
+    g = GroupTiles<HEIGHT>(a, base, row, tiles);
+  }
+  const int rows = (int)a.rows, behind = row, first_behind = tiles;
+  const int tile = tile_of(tiles + (rows - row + HEIGHT - 1) / HEIGHT);
+  if (tile < 0) return {0, 0, 0};
+  if (tile >= first_behind) {
+    const int at = behind + (tile - first_behind) * HEIGHT;
+    return {at, min(at + HEIGHT, rows), -1};
+  }
+  if (base > 0) g = GroupTiles<HEIGHT>(a, base = 0, 0, 0);
+  for (;;) {
+    const unsigned long long here = __ballot(tile < g.tiles_with);
+    if (here != 0) {
+      const int owner = __builtin_ctzll(here);
+      const int at = __builtin_amdgcn_readlane(g.first, owner) + (tile - __builtin_amdgcn_readlane(g.tiles_before, owner)) * HEIGHT;
+      return {at, min(at + HEIGHT, __builtin_amdgcn_readlane(g.end, owner)), base + owner};
+    }
+    base += 64;                                                  // (tile < first_behind: some group has it)
+    g = GroupTiles<HEIGHT>(a, base, __builtin_amdgcn_readlane(g.end, 63), __builtin_amdgcn_readlane(g.tiles_with, 63));
+  }
 }
 
 // The row of x behind row `row` of the outputs; -1: none, a row of zeros.
@@ -177,13 +218,13 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs &a, int64_t row)
 // A work-group computes 16 MT rows x 16 NT columns from global memory straight into registers; its waves take the blocks of k in turn,
 // and their sums meet in LDS in the waves' order.
 template <int MT, int NT, bool EXACT, bool GROUPED>
-__global__ __launch_bounds__(MT * NT == 1 ? 1024 : 512) void lutkan_fp8_direct_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_kernel(const ProductArgs a) {
   extern __shared__ __align__(16) f32x4 s_part[];                // [wave][row tile][column tile][lane]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int p = lane >> 4, col0 = blockIdx.x * (16 * NT);
   RowTile t;
   if constexpr (GROUPED) {
-    t = grouped_tile(a, blockIdx.y, 16 * MT);
+    t = grouped_tile<16 * MT>(a, [&](int tiles) { return (int)blockIdx.y < tiles ? (int)blockIdx.y : -1; });
     if (t.end <= t.first) return;
   } else {
     t.first = (int64_t)blockIdx.y * (16 * MT);
@@ -208,30 +249,46 @@ __global__ __launch_bounds__(MT * NT == 1 ? 1024 : 512) void lutkan_fp8_direct_k
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) w[n] = a.w + t.group * a.w_matrix_stride + (int64_t)min(col0 + 16 * n + (lane & 15), a.n - 1) * a.w_stride;
-    const auto block = [&](int b, auto at_end) {
-      i32x8 wc[NT], xc[MT];
+    // Codes and scales of a block, and its products: kDepth blocks are read before the first is multiplied.
+    constexpr int kDepth = MT * NT == 1 ? 4 : MT * NT == 2 ? 2 : 1;
+    struct Block { i32x8 w[NT], x[MT]; float scale[MT]; };
+    const auto read = [&](Block &to, int b, auto at_end) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) wc[n] = block_of_row<decltype(at_end)::value>(w[n], b * kScaleBlock, p, a.k);
-#pragma unroll
-      for (int m = 0; m < MT; ++m) xc[m] = block_of_row<decltype(at_end)::value>(x[m], b * kScaleBlock, p, a.k);
-      Operand<EXACT> wf[NT], xf;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) wf[n].set(wc[n]);
+      for (int n = 0; n < NT; ++n) to.w[n] = block_of_row<decltype(at_end)::value>(w[n], b * kScaleBlock, p, a.k);
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const float scale = xs[m][b] * ws[b];
-        xf.set(xc[m]);
+        to.x[m] = block_of_row<decltype(at_end)::value>(x[m], b * kScaleBlock, p, a.k);
+        to.scale[m] = xs[m][b] * ws[b];
+      }
+    };
+    const auto multiply = [&](const Block &of) {
+      Operand<EXACT> wf[NT], xf;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) wf[n].set(of.w[n]);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        xf.set(of.x[m]);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const f32x4 v = block_product(wf[n], xf);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[m][n][e] = fmaf(scale, v[e], acc[m][n][e]);
+          for (int e = 0; e < 4; ++e) acc[m][n][e] = fmaf(of.scale[m], v[e], acc[m][n][e]);
         }
       }
     };
     const int whole = a.k / kScaleBlock;
-    for (int b = wave; b < whole; b += waves) block(b, std::false_type{});
-    if (whole < a.k_blocks && whole % waves == wave) block(whole, std::true_type{});
+    for (int b = wave; b < whole; b += waves * kDepth) {
+      Block held[kDepth];
+#pragma unroll
+      for (int d = 0; d < kDepth; ++d) if (b + d * waves < whole) read(held[d], b + d * waves, std::false_type{});
+#pragma unroll
+      for (int d = 0; d < kDepth; ++d) if (b + d * waves < whole) multiply(held[d]);
+    }
+    if (whole < a.k_blocks && whole % waves == wave) {
+      Block last;
+      read(last, whole, std::true_type{});
+      multiply(last);
+    }
   } else {
 #pragma unroll
     for (int m = 0; m < MT; ++m) none[m] = true;
@@ -260,47 +317,78 @@ __global__ __launch_bounds__(MT * NT == 1 ? 1024 : 512) void lutkan_fp8_direct_k
 }
 
 template <int MT, int NT, bool EXACT, bool GROUPED>
-void launch_direct(const ProductArgs &a, int64_t row_tiles, int waves, hipStream_t s) {
+int launch_direct(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
+  if (row_tiles > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
+  const int waves = std::min(a.k_blocks, 16);
   const dim3 grid((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)row_tiles);
+  lutkan::plan_note("fp8_direct rows=%d columns=%d waves=%d; ", 16 * MT, 16 * NT, waves);
   hipLaunchKernelGGL((lutkan_fp8_direct_kernel<MT, NT, EXACT, GROUPED>), grid, dim3(64 * waves), waves > 1 ? (size_t)waves * MT * NT * 64 * sizeof(f32x4) : 0, s, a);
+  return check_launch(who);
 }
 
-// A tile of 16 MT WM rows x 16 NT WN columns for a work-group of WM x WN waves, each 16 MT rows x 16 NT columns of it.  Both operands'
-// blocks of k go through LDS, in two buffers of 128 bytes a row: while a block is multiplied the next is on its way.  A row's eight
-// 16-byte pieces lie in an order that depends on the row (piece_place), so that the 16 rows that a read of 16 lanes takes lie in
-// different banks.
-//   ASYNC: the pieces go from global memory to LDS without passing through registers: needs 16-byte aligned rows and offsets
-//   that fit 32 bits.  Otherwise, and for a last block that is not whole, through registers.
+// A tile of 16 MT WM rows x 16 NT WN columns for a work-group of KG teams of WM x WN waves, each wave 16 MT rows x 16 NT columns of it.
+// The teams take the blocks of k in turn; their sums meet in LDS in the teams' order.  A team's blocks (both operands' codes and their
+// scales) go through LDS, in STAGES buffers: while a block is multiplied the next STAGES - 1 are on their way.  A row's eight 16-byte pieces lie in an order that depends on the row (piece_place), so that the 16 rows that a read of 16 lanes takes
+// lie in different banks (no conflict counted).
+//   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and
+//   offsets that fit 32 bits.  Otherwise, and for a last block that is not whole, through registers.
 __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ ((row >> 1) & 7); }
 
-template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED, bool ASYNC>
-__global__ __launch_bounds__(64 * WM * WN, 512 / (64 * WM * WN)) void lutkan_fp8_tiled_kernel(const ProductArgs a, unsigned row_tiles) {
-  constexpr int kRows = 16 * MT * WM, kCols = 16 * NT * WN, kWaves = WM * WN, kThreads = 64 * kWaves, kStage = (kRows + kCols) * kScaleBlock;
-  constexpr int kXCopies = kRows / 8 / kWaves, kWCopies = kCols / 8 / kWaves;          // of 8 rows, for each wave
-  static_assert(kXCopies * 8 * kWaves == kRows && kWCopies * 8 * kWaves == kCols && kThreads >= kRows && kScaleBlock % (16 * NT) == 0, "tile");
-  extern __shared__ __align__(16) unsigned char s_tiles[];       // [buffer][rows of x, rows of the weight][128], then [buffer][threads] scales
-  float *s_scales = reinterpret_cast<float *>(s_tiles + 2 * kStage);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN, p = lane >> 4;
+// As copy16_global_to_lds_at, four bytes a lane.
+__device__ __forceinline__ void copy4_global_to_lds_at(const void *uniform_base, unsigned lane_byte_offset, void *lds_dst) {
+  const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)lds_dst);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(lane_byte_offset), "s"(uniform_base) : "m0", "memory");
+}
+
+// Waits until at most N of the wave's vector memory loads are outstanding (they end in the order in which they began).
+template <int N>
+__device__ __forceinline__ void wait_vector_loads() {
+  static_assert(N < 64, "a six-bit counter");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+}
+
+// The sizes of a tile, its buffers and its team.
+template <int MT, int NT, int WM, int WN, int KG, int STAGES>
+struct Tile {
+  static constexpr int kRows = 16 * MT * WM, kCols = 16 * NT * WN, kThreads = 64 * WM * WN;
+  static constexpr int kScalesAt = (kRows + kCols) * kScaleBlock, kStage = kScalesAt + (kRows + 4) * 4;      // codes, scales of the rows, of the columns' blocks
+  static constexpr int kParts = KG > 1 ? (KG - 1) * kRows * kCols * 4 : 0;       // the sums of all teams but the one that adds them up
+  static constexpr int kLds = KG * STAGES * kStage > kParts ? KG * STAGES * kStage : kParts;
+  static_assert(kLds <= lutkan::kLdsPerWorkGroup && kStage % 16 == 0, "LDS");
+};
+
+template <int MT, int NT, int WM, int WN, int KG, int STAGES, bool EXACT, bool GROUPED, bool ASYNC>
+__global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void lutkan_fp8_tiled_kernel(const ProductArgs a, unsigned row_tiles) {
+  using T = Tile<MT, NT, WM, WN, KG, STAGES>;
+  constexpr int kRows = T::kRows, kCols = T::kCols, kWaves = WM * WN, kThreads = T::kThreads, kScalesAt = T::kScalesAt, kStage = T::kStage;
+  constexpr int kXCopies = kRows / 8 / kWaves, kWCopies = kCols / 8 / kWaves, kCopies = kXCopies + kWCopies;     // of 8 rows, for each wave
+  static_assert(kXCopies * 8 * kWaves == kRows && kWCopies * 8 * kWaves == kCols && kXCopies % 2 == 0 && kWCopies % 2 == 0, "copies in pairs");
+  static_assert(kThreads >= kRows && kScaleBlock % (16 * NT) == 0 && (STAGES & (STAGES - 1)) == 0 && (ASYNC || STAGES == 2), "tile");
+  extern __shared__ __align__(16) unsigned char s_tiles[];       // [team][stage][rows of x, rows of the weight][128], scales
+  const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave_of_all / kWaves;
+  const int wave = wave_of_all % kWaves, tid = wave * 64 + lane, wm = wave / WN, wn = wave % WN, p = lane >> 4;
   // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, and in a run eight row tiles share a column
   // tile before the next, so that what an XCD's work-groups read at a time meets in its L2.
   const unsigned col_tiles = (a.n + kCols - 1) / kCols;
-  if constexpr (GROUPED) row_tiles = (unsigned)uniform(grouped_tiles(a, kRows));
-  const unsigned tiles = row_tiles * col_tiles;
-  if (blockIdx.x >= tiles) return;
-  const unsigned xcd = blockIdx.x % 8, of_xcd = tiles / 8, more = tiles % 8;
-  const unsigned tile = xcd * of_xcd + min(xcd, more) + blockIdx.x / 8;
-  const unsigned band = tile / (8 * col_tiles), in_band = tile - band * 8 * col_tiles, high = min(8u, row_tiles - band * 8);
-  const unsigned row_tile = band * 8 + in_band % high;
-  const int col0 = (int)(in_band / high) * kCols;
+  int col0 = 0;
+  const auto tile_of = [&](unsigned row_tiles) {                 // the row tile; sets the column
+    const unsigned tiles = row_tiles * col_tiles;
+    if (blockIdx.x >= tiles) return -1;
+    const unsigned xcd = blockIdx.x % 8, of_xcd = tiles / 8, more = tiles % 8;
+    const unsigned tile = xcd * of_xcd + min(xcd, more) + blockIdx.x / 8;
+    const unsigned band = tile / (8 * col_tiles), in_band = tile - band * 8 * col_tiles, high = min(8u, row_tiles - band * 8);
+    col0 = (int)(in_band / high) * kCols;
+    return (int)(band * 8 + in_band % high);
+  };
   RowTile t;
   if constexpr (GROUPED) {
-    t = grouped_tile(a, row_tile, kRows);
-    t.first = uniform(t.first); t.end = uniform(t.end); t.group = __builtin_amdgcn_readfirstlane(t.group);
+    t = grouped_tile<kRows>(a, tile_of);
   } else {
-    t.first = (int64_t)row_tile * kRows;
+    t.first = (int64_t)tile_of(row_tiles) * kRows;               // (the grid has as many work-groups as there are tiles)
     t.end = min(t.first + kRows, a.rows);
     t.group = 0;
   }
+  if (t.end <= t.first) return;
   f32x4 acc[MT][NT];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -309,77 +397,94 @@ __global__ __launch_bounds__(64 * WM * WN, 512 / (64 * WM * WN)) void lutkan_fp8
   if (t.group >= 0) {
     const unsigned char *w_tile = a.w + t.group * a.w_matrix_stride + (int64_t)col0 * a.w_stride;
     const unsigned char *x_tile = GROUPED ? a.x : a.x + t.first * a.x_stride;
+    const float *scales_tile = GROUPED ? a.x_scales : a.x_scales + t.first * a.x_scales_stride;
     typedef std::conditional_t<ASYNC, unsigned, int64_t> offset_t;
-    offset_t x_from[kXCopies], w_from[kWCopies];                 // the rows that this lane's pieces come from
+    offset_t x_from[kXCopies], w_from[kWCopies], scale_from;     // the rows that this lane's pieces, and its scale, come from
     int piece_at[2];                                             // and the columns: place i of row r, the same for every 16 rows
 #pragma unroll
     for (int c = 0; c < 2; ++c) piece_at[c] = piece_place(c * 8 + (lane >> 3), lane & 7) * 16;        // (its own inverse)
-    static_assert(kXCopies % 2 == 0 && kWCopies % 2 == 0, "copies in pairs");
+    const auto row_of = [&](int r) {                             // rows behind the last are the last again
+      const int64_t row = min(t.first + r, t.end - 1);
+      return GROUPED ? max(source_row<GROUPED>(a, row), (int64_t)0) : row - t.first;
+    };
 #pragma unroll
-    for (int c = 0; c < kXCopies; ++c) {
-      const int64_t row = min(t.first + (wave * kXCopies + c) * 8 + (lane >> 3), t.end - 1);
-      x_from[c] = (offset_t)((GROUPED ? max(source_row<GROUPED>(a, row), (int64_t)0) : row - t.first) * a.x_stride);
-    }
+    for (int c = 0; c < kXCopies; ++c) x_from[c] = (offset_t)(row_of((wave * kXCopies + c) * 8 + (lane >> 3)) * a.x_stride);
 #pragma unroll
     for (int c = 0; c < kWCopies; ++c) w_from[c] = (offset_t)((int64_t)min((wave * kWCopies + c) * 8 + (lane >> 3), a.n - 1 - col0) * a.w_stride);
-    const int64_t scale_row = min(t.first + min(tid, kRows - 1), t.end - 1);
-    const float *xs = a.x_scales + max(source_row<GROUPED>(a, scale_row), (int64_t)0) * a.x_scales_stride;
-    const float *ws = a.w_scales + ((int64_t)t.group * a.n_blocks + min(col0 + wn * 16 * NT, a.n - 1) / kScaleBlock) * a.k_blocks;
-    const int whole = a.k / kScaleBlock;
-    u32x4 held[ASYNC ? 1 : kXCopies + kWCopies];
-    // Block b's pieces are asked for, and put into a buffer: at once where they go straight there, else by put().
-    const auto ask = [&](int b) {
+    scale_from = (offset_t)(row_of(min(tid, kRows - 1)) * a.x_scales_stride * 4);
+    constexpr int kColBlocks = kCols > kScaleBlock ? kCols / kScaleBlock : 1;    // (a tile of fewer columns lies in one block)
+    const float *w_scales_tile = a.w_scales + ((int64_t)t.group * a.n_blocks + col0 / kScaleBlock) * a.k_blocks;
+    const unsigned w_scale_from = (unsigned)(min(lane, a.n_blocks - 1 - col0 / kScaleBlock) * a.k_blocks) * 4;
+    const int whole = a.k / kScaleBlock, own = (whole - team + KG - 1) / KG, steps = (whole + KG - 1) / KG;     // whole blocks: all, this team's, the first team's
+    unsigned char *const s_team = s_tiles + team * STAGES * kStage;
+    const auto block_of = [&](int step) { return step * KG + team; };
+    const auto stage = [&](int step) { return s_team + (step & (STAGES - 1)) * kStage; };
+    u32x4 held[ASYNC ? 1 : kCopies];
+    // The pieces of this team's block of a step are asked for, copy by copy, and put into their buffer: at once where they go straight
+    // there, else by put().
+    const auto ask = [&](int step, int c) {
+      const bool of_x = c < kXCopies;
+      const int cw = c - kXCopies;
+      const int64_t b = block_of(step);
       if constexpr (ASYNC) {
-        unsigned char *to = s_tiles + (b & 1) * kStage;
-#pragma unroll
-        for (int c = 0; c < kXCopies; ++c) copy16_global_to_lds_at(x_tile + (int64_t)b * kScaleBlock, x_from[c] + piece_at[c & 1], to + (wave * kXCopies + c) * 1024);
-#pragma unroll
-        for (int c = 0; c < kWCopies; ++c)
-          copy16_global_to_lds_at(w_tile + (int64_t)b * kScaleBlock, w_from[c] + piece_at[c & 1], to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024);
+        unsigned char *to = stage(step) + (of_x ? (wave * kXCopies + c) * 1024 : kRows * kScaleBlock + (wave * kWCopies + cw) * 1024);
+        copy16_global_to_lds_at((of_x ? x_tile : w_tile) + b * kScaleBlock, (of_x ? x_from[c] : w_from[cw]) + piece_at[c & 1], to);
+        if (c == 0 && wave < kRows / 64) copy4_global_to_lds_at(scales_tile + b, scale_from, stage(step) + kScalesAt + wave * 256);
+        if (c == 0 && wave == kWaves - 1 && lane < kColBlocks) copy4_global_to_lds_at(w_scales_tile + b, w_scale_from, stage(step) + kScalesAt + kRows * 4);
       } else {
-#pragma unroll
-        for (int c = 0; c < kXCopies; ++c) held[c] = load_any<u32x4>(x_tile + x_from[c] + (b * kScaleBlock + piece_at[c & 1]));
-#pragma unroll
-        for (int c = 0; c < kWCopies; ++c) held[kXCopies + c] = load_any<u32x4>(w_tile + w_from[c] + (b * kScaleBlock + piece_at[c & 1]));
+        held[c] = load_any<u32x4>((of_x ? x_tile + x_from[c] : w_tile + w_from[cw]) + (b * kScaleBlock + piece_at[c & 1]));
       }
     };
-    const auto put = [&](int b) {
+    const auto put_scales = [&](int step, int b) {
+      float *to = reinterpret_cast<float *>(stage(step) + kScalesAt);
+      if (tid < kRows) to[tid] = load_any<float>(reinterpret_cast<const unsigned char *>(scales_tile + b) + scale_from);
+      if (tid < kColBlocks) to[kRows + tid] = load_any<float>(reinterpret_cast<const unsigned char *>(w_scales_tile + b) + w_scale_from);
+    };
+    const auto put = [&](int step) {
       if constexpr (!ASYNC) {
-        unsigned char *to = s_tiles + (b & 1) * kStage + lane * 16;
+        unsigned char *to = stage(step) + lane * 16;
 #pragma unroll
         for (int c = 0; c < kXCopies; ++c) *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = held[c];
 #pragma unroll
         for (int c = 0; c < kWCopies; ++c) *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = held[kXCopies + c];
+        put_scales(step, block_of(step));
       }
     };
-    // The last block, if it is not whole.
+    // The last block, if it is not whole: this team's step `own`.
     const auto put_end = [&]() {
-      unsigned char *to = s_tiles + (whole & 1) * kStage + lane * 16;
+      unsigned char *to = stage(own) + lane * 16;
       for (int c = 0; c < kXCopies; ++c)
         *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = piece_at_end(x_tile + x_from[c], whole * kScaleBlock + piece_at[c & 1], a.k);
       for (int c = 0; c < kWCopies; ++c)
         *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = piece_at_end(w_tile + w_from[c], whole * kScaleBlock + piece_at[c & 1], a.k);
+      put_scales(own, whole);
     };
     const int at_row = lane & 15, low = at_row * kScaleBlock + piece_place(at_row, p) * 16, high_half = at_row * kScaleBlock + piece_place(at_row, p + 4) * 16;
     // One block: the products in a fixed order, each added two products after it was begun; a row subtile's codes are read while the one
     // before it is multiplied.
-    const auto multiply = [&](int b, float w_scale) {
-      const unsigned char *xt = s_tiles + (b & 1) * kStage + (wm * 16 * MT) * kScaleBlock;
-      const unsigned char *wt = s_tiles + (b & 1) * kStage + (kRows + wn * 16 * NT) * kScaleBlock;
-      const float *scales = s_scales + (b & 1) * kThreads + wm * 16 * MT + at_row;
+    const auto multiply = [&](int step, bool ask_more) {
+      const unsigned char *xt = stage(step) + (wm * 16 * MT) * kScaleBlock;
+      const unsigned char *wt = stage(step) + (kRows + wn * 16 * NT) * kScaleBlock;
+      const float *scales = reinterpret_cast<const float *>(stage(step) + kScalesAt) + wm * 16 * MT + at_row;
+      const float w_scale = scales[kRows + wn * 16 * NT / kScaleBlock - (wm * 16 * MT + at_row)];
       const auto codes = [&](const unsigned char *rows, int sub) {
         return fragment(*reinterpret_cast<const u32x4 *>(rows + sub * 16 * kScaleBlock + low), *reinterpret_cast<const u32x4 *>(rows + sub * 16 * kScaleBlock + high_half));
       };
-      Operand<EXACT> wf[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) wf[n].set(codes(wt, n));
-      i32x8 next = codes(xt, 0);
+      i32x8 next = codes(xt, 0), wc[NT];
       float next_scale = scales[0];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {                             // in the order of their first products
+        wc[n] = codes(wt, n);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      Operand<EXACT> wf[NT];
       Operand<EXACT> xf;
-      f32x4 v[3];
+      constexpr int kAhead = 2, kEvery = MT * NT / kCopies >= 2 ? 2 : 1;
+      static_assert(kEvery * kCopies <= MT * NT, "copies");
+      f32x4 v[kAhead + 1];
       float scales_of[2];
 #pragma unroll
-      for (int i = 0; i < MT * NT + 2; ++i) {
+      for (int i = 0; i < MT * NT + kAhead; ++i) {
         const int m = i / NT, n = i % NT;
         if (i < MT * NT) {
           if (n == 0) {
@@ -390,95 +495,148 @@ __global__ __launch_bounds__(64 * WM * WN, 512 / (64 * WM * WN)) void lutkan_fp8
               next_scale = scales[(m + 1) * 16];
             }
           }
-          v[i % 3] = block_product(wf[n], xf);
+          if (m == 0) wf[n].set(wc[n]);
+          v[i % (kAhead + 1)] = block_product(wf[n], xf);
+          __builtin_amdgcn_sched_barrier(0);
+          // Copies in between: a wave waits for its turn with each, and all at once would keep it from its products.
+          if (i % kEvery == kEvery - 1 && i / kEvery < kCopies && ask_more) ask(step + STAGES - 1, i / kEvery);
         }
-        if (i >= 2) {
-          const int of = i - 2;
+        if (i >= kAhead) {
+          const int of = i - kAhead;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[of / NT][of % NT][e] = fmaf(scales_of[(of / NT) & 1], v[of % 3][e], acc[of / NT][of % NT][e]);
+          for (int e = 0; e < 4; ++e) acc[of / NT][of % NT][e] = fmaf(scales_of[(of / NT) & 1], v[of % (kAhead + 1)][e], acc[of / NT][of % NT][e]);
           asm volatile("" : "+v"(acc[of / NT][of % NT]));        // (here, not behind the next branch, with all products held until then)
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    float scale = xs[0], w_scale = ws[0];
-    if (whole > 0) {
-      ask(0);
-      put(0);
-    }
-    s_scales[tid] = scale;                                       // (threads beyond the rows: the last row's again, behind the others)
-    for (int b = 0; b < whole; ++b) {
-      wait_all_vector_loads();
-      lds_barrier();                                             // block b is there, and nobody reads the other buffer any more
-      scale = xs[min(b + 1, a.k_blocks - 1)];                    // (before the copies: a wait for these does not have to wait for them)
-      const float next_w_scale = ws[min(b + 1, a.k_blocks - 1)];
-      if (b + 1 < whole) ask(b + 1);
-      multiply(b, w_scale);
-      w_scale = next_w_scale;
-      if (b + 1 < whole) put(b + 1);
-      s_scales[((b + 1) & 1) * kThreads + tid] = scale;
+#pragma unroll
+    for (int step = 0; step < STAGES - 1; ++step)
+      if (step < own)
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) ask(step, c);
+    if (own > 0) put(0);
+    for (int step = 0; step < steps; ++step) {
+      // The block is there when no more than the copies of the blocks behind it are outstanding (a wave that also copies scales waits
+      // for a few more than it has to).
+      if (step + STAGES - 1 <= own) wait_vector_loads<(STAGES - 2) * kCopies>();
+      else wait_vector_loads<0>();
+      lds_barrier();                                             // ... every wave's part of it, and nobody reads the buffer of the block before it any more
+      if (step < own) multiply(step, step + STAGES - 1 < own);
+      if (step + 1 < own) put(step + 1);
     }
     if (whole < a.k_blocks) {
-      put_end();                                                 // (into the buffer that nobody reads since the last barrier)
+      const bool mine = whole % KG == team;
+      if (mine) put_end();                                       // (into a buffer that nobody reads since the last barrier)
       lds_barrier();
-      multiply(whole, w_scale);
+      if (mine) multiply(own, false);
+    }
+    if constexpr (KG > 1) {
+      lds_barrier();                                             // nobody reads the buffers any more
+      f32x4 *parts = reinterpret_cast<f32x4 *>(s_tiles);         // [team - 1][wave][m][n][lane]
+      if (team > 0) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) parts[((((team - 1) * kWaves + wave) * MT + m) * NT + n) * 64 + lane] = acc[m][n];
+      }
+      lds_barrier();
+      if (team > 0) return;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          for (int o = 0; o < KG - 1; ++o) acc[m][n] += parts[(((o * kWaves + wave) * MT + m) * NT + n) * 64 + lane];
     }
   }
+  if (KG > 1 && team > 0) return;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int64_t row = t.first + (wm * MT + m) * 16 + (lane & 15);
-    if (row >= t.end) continue;
-    const bool none = t.group < 0 || source_row<GROUPED>(a, row) < 0;
+    const bool none = t.group < 0 || (GROUPED && row < t.end && source_row<GROUPED>(a, row) < 0);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) store_outputs(a, row, col0 + (wn * NT + n) * 16 + 4 * p, none ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[m][n]);
+    for (int n = 0; n < NT; ++n) acc[m][n] = none ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[m][n];
+    store_row<NT>(a, row, row < t.end, col0 + wn * NT * 16, p, acc[m]);
   }
 }
 
-template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED, bool ASYNC>
-int launch_tiled(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
-  constexpr int kRows = 16 * MT * WM, kCols = 16 * NT * WN;
-  constexpr int kLds = 2 * (kRows + kCols) * kScaleBlock + 2 * 64 * WM * WN * (int)sizeof(float);
+template <int MT, int NT, int WM, int WN, int KG, int STAGES, bool EXACT, bool GROUPED, bool ASYNC>
+int launch_tiles(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
+  using T = Tile<MT, NT, WM, WN, KG, STAGES>;
   static LdsCap cap;
-  const auto kernel = lutkan_fp8_tiled_kernel<MT, NT, WM, WN, EXACT, GROUPED, ASYNC>;
+  const auto kernel = lutkan_fp8_tiled_kernel<MT, NT, WM, WN, KG, STAGES, EXACT, GROUPED, ASYNC>;
   if (int rc = raise_lds_cap(kernel, &cap, who)) return rc;
-  lutkan::plan_note("fp8_tiled rows=%d columns=%d%s; ", kRows, kCols, ASYNC ? " async" : "");
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * ((a.n + kCols - 1) / kCols))), dim3(64 * WM * WN), kLds, s, a, (unsigned)row_tiles);
+  lutkan::plan_note("fp8_tiled rows=%d columns=%d teams=%d stages=%d%s; ", T::kRows, T::kCols, KG, STAGES, ASYNC ? " async" : "");
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * ((a.n + T::kCols - 1) / T::kCols))), dim3(T::kThreads * KG), T::kLds, s, a, (unsigned)row_tiles);
   return check_launch(who);
 }
 
-template <int MT, int NT, int WM, int WN, bool EXACT, bool GROUPED>
-int launch_tiled(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
-  const int64_t x_span = (GROUPED ? a.x_rows : 16 * MT * WM) * a.x_stride, w_span = 16 * NT * WN * a.w_stride;
-  const bool async = ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 15) == 0 &&
-                     x_span < ((int64_t)1 << 32) && w_span < ((int64_t)1 << 32);
-  return async ? launch_tiled<MT, NT, WM, WN, EXACT, GROUPED, true>(a, row_tiles, who, s) : launch_tiled<MT, NT, WM, WN, EXACT, GROUPED, false>(a, row_tiles, who, s);
+// Rows at dword addresses, as global loads of several dwords ask for, and at offsets that the copies can hold.
+template <bool GROUPED>
+bool copies_async(const ProductArgs &a) {
+  const int64_t x_span = GROUPED ? a.x_rows : 256, most = (int64_t)1 << 32;
+  return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 3) == 0 &&
+         a.x_stride < most / x_span && a.x_scales_stride < most / 4 / x_span && a.w_stride < most / 256;
+}
+
+// What a launch takes beyond an empty one, in us, for the kernels' choice; fitted to times from 1 to 8192 rows, 128 to 8192 inputs and
+// 256 to 8192 outputs (within a fifth of them where two kernels come near each other).
+//   direct   what its work-groups read, each its own: 9 MB/us over the whole GPU
+//   tiled    rounds of as many tiles as fit the compute units, a tile's steps over k: `one` where there is one to a compute unit, `all` where
+//            there are `slots`, and `ends` before and behind the steps
+inline double direct_price(double row_tiles, double rows_of_tile, int columns, const ProductArgs &a) {
+  const double work_groups = row_tiles * ((a.n + columns - 1) / columns);
+  return work_groups * (rows_of_tile + columns) * a.k / (9e6 * std::min(1.0, work_groups / 256));
+}
+inline double tiled_price(double tiles, int slots, double one, double all, double ends, double steps) {
+  const double full = std::floor(tiles / (256 * slots)), rest = tiles - full * 256 * slots;
+  return full * (steps * all + ends) + (rest > 0 ? steps * (rest <= 256 ? one : all) + ends : 0);
 }
 
 template <bool EXACT, bool GROUPED>
 int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
-  const int groups = GROUPED ? a.groups : 1;
+  const int64_t groups = GROUPED ? a.groups : 1;
   const auto tiles = [&](int height) {                           // no routing has more
     return GROUPED ? a.rows / height + std::min<int64_t>(groups + 1, a.rows) : (a.rows + height - 1) / height;
   };
+  const auto likely_tiles = [&](int height) {                    // of a routing of some spread: a group's last tile is half empty
+    if (!GROUPED) return (double)tiles(height);
+    const double some = (double)std::min(groups, a.rows), each = (double)a.rows / some;
+    return some * std::max(1.0, each / height + (each > 1 ? 0.6 : 0.0));
+  };
   if (tiles(64) * ((a.n + 63) / 64) > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   lutkan::plan_clear();
-  const int64_t large = tiles(256) * ((a.n + 255) / 256);        // (at least three quarters of the compute units get a tile)
-  int pick = a.rows <= 32 * (int64_t)groups ? 0 : a.rows < 128 * (int64_t)groups ? 1 : EXACT || large < 192 ? 2 : 3;
-  if (pick == 0) {
-    if (tiles(16) > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
-    const int waves = std::max(1, std::min(a.k_blocks, 16));
-    lutkan::plan_note("fp8_direct rows=16 columns=16 waves=%d; ", waves);
-    launch_direct<1, 1, EXACT, GROUPED>(a, tiles(16), waves, s);
-  } else if (pick == 1) {
-    if (tiles(64) > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
-    const int waves = std::max(1, std::min(a.k_blocks, 4));
-    lutkan::plan_note("fp8_direct rows=64 columns=64 waves=%d; ", waves);
-    launch_direct<4, 4, EXACT, GROUPED>(a, tiles(64), waves, s);
-  } else {
-    if constexpr (EXACT) return launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), who, s);
-    else return pick == 2 ? launch_tiled<4, 4, 2, 2, EXACT, GROUPED>(a, tiles(128), who, s) : launch_tiled<8, 4, 2, 4, EXACT, GROUPED>(a, tiles(256), who, s);
+  const bool async = copies_async<GROUPED>(a);
+  const double likely_rows = (double)a.rows / (double)std::min(groups, a.rows), k_blocks = a.k_blocks;
+  const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
+    return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one, all, ends, std::ceil(k_blocks / teams));
+  };
+  enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kKernels };
+  double price[kKernels];
+  price[kDirect16x16] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 16, a);
+  price[kDirect16x32] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 32, a);
+  price[kDirect32x32] = direct_price(likely_tiles(32), std::min(32.0, likely_rows), 32, a);
+  price[kTiled64x4] = EXACT ? tiled(64, 1, 1.05, 1.4, 1, 4) : tiled(64, 1, 0.62, 1.0, 1, 4);
+  price[kTiled64x2] = EXACT ? tiled(64, 2, 0.62, 1.3, 1, 2) : tiled(64, 2, 0.36, 0.85, 1, 2);
+  price[kTiled128x2] = EXACT ? tiled(128, 1, 1.75, 1.75, 5, 2) : tiled(128, 1, 1.0, 1.0, 5, 2);
+  price[kTiled128] = EXACT ? tiled(128, 2, 1.3, 1.9, 2, 1) : tiled(128, 2, 0.65, 1.08, 2, 1);
+  price[kTiled256] = EXACT ? HUGE_VAL : tiled(256, 1, 1.6, 1.6, 6, 1);
+  if (!async)                                                    // (through registers: one kernel of the tiled ones)
+    for (int k : {kTiled64x4, kTiled64x2, kTiled128x2, kTiled256}) price[k] = HUGE_VAL;
+  if (tiles(16) > 65535) price[kDirect16x16] = price[kDirect16x32] = HUGE_VAL;
+  if (tiles(32) > 65535) price[kDirect32x32] = HUGE_VAL;
+  const int pick = (int)(std::min_element(price, price + kKernels) - price);
+  switch (pick) {
+    case kDirect16x16: return launch_direct<1, 1, EXACT, GROUPED>(a, tiles(16), who, s);
+    case kDirect16x32: return launch_direct<1, 2, EXACT, GROUPED>(a, tiles(16), who, s);
+    case kDirect32x32: return launch_direct<2, 2, EXACT, GROUPED>(a, tiles(32), who, s);
+    case kTiled64x4: return launch_tiles<2, 2, 2, 2, 4, 2, EXACT, GROUPED, true>(a, tiles(64), who, s);
+    case kTiled64x2: return launch_tiles<2, 2, 2, 2, 2, 2, EXACT, GROUPED, true>(a, tiles(64), who, s);
+    case kTiled128x2: return launch_tiles<4, 4, 2, 2, 2, 2, EXACT, GROUPED, true>(a, tiles(128), who, s);
+    case kTiled256: if constexpr (!EXACT) return launch_tiles<8, 4, 2, 4, 1, 2, EXACT, GROUPED, true>(a, tiles(256), who, s);
+    default: break;
   }
-  return check_launch(who);
+  return async ? launch_tiles<4, 4, 2, 2, 1, 2, EXACT, GROUPED, true>(a, tiles(128), who, s) : launch_tiles<4, 4, 2, 2, 1, 2, EXACT, GROUPED, false>(a, tiles(128), who, s);
 }
 
 int check_product(const lutkan_matmul_fp8_args *p, const char *who, ProductArgs *a) {
@@ -522,6 +680,7 @@ extern "C" int lutkan_grouped_matmul_fp8(const lutkan_matmul_fp8_args *p, void *
   if (!p->group_sizes) return fail(LUTKAN_EINVAL, "%s: null group_sizes", who);
   if ((p->group_sizes_bytes != 4 && p->group_sizes_bytes != 8) || (p->row_index && p->row_index_bytes != 4 && p->row_index_bytes != 8))
     return fail(LUTKAN_EINVAL, "%s: group_sizes and row_index are whole numbers of 4 or 8 bytes", who);
+  if (p->rows > LUTKAN_FP8_MAX_GROUPED_ROWS) return fail(LUTKAN_EUNSUPPORTED, "%s: %lld rows, at most %d", who, (long long)p->rows, LUTKAN_FP8_MAX_GROUPED_ROWS);
   if (!p->row_index && p->rows != p->x_rows) return fail(LUTKAN_ESHAPE, "%s: %lld rows out, %lld in, and no row_index", who, (long long)p->rows, (long long)p->x_rows);
   if (p->row_index && p->x_rows == 0) return fail(LUTKAN_ESHAPE, "%s: row_index into no rows", who);
   a.group_sizes = p->group_sizes; a.row_index = p->row_index; a.groups = p->groups;
