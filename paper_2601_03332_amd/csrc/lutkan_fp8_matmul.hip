@@ -22,16 +22,22 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+// A launch whose arguments take at most 112 bytes costs the host 2.8 us, one with 160 bytes 3.5: lengths and strides travel in 32 bits.
 struct ProductArgs {
   const unsigned char *x, *w;
   const float *x_scales, *w_scales;
   unsigned char *y;
-  int64_t x_rows, x_stride, x_scales_stride, w_stride, w_matrix_stride, y_stride;    // bytes of codes, elements of scales and outputs
-  int64_t rows;
-  int32_t k, n, k_blocks, n_blocks, y_type;
   const void *group_sizes, *row_index;
-  int32_t groups, group_sizes_bytes, row_index_bytes;
+  int64_t w_matrix_stride;
+  int32_t x_stride, x_scales_stride, w_stride, y_stride;                             // bytes of codes, elements of scales and outputs
+  int32_t rows, x_rows, k, n, groups;
+  int8_t y_type, group_sizes_bytes, row_index_bytes;
+  int32_t extent;                                                                    // direct: waves of a work-group; tiled: row tiles
+
+  __host__ __device__ int k_blocks() const { return (k + kScaleBlock - 1) / kScaleBlock; }
+  __host__ __device__ int n_blocks() const { return (n + kScaleBlock - 1) / kScaleBlock; }
 };
+static_assert(sizeof(ProductArgs) <= 112, "launch");
 
 __device__ __forceinline__ i32x8 fragment(u32x4 low, u32x4 high) {
   return i32x8{(int)low.x, (int)low.y, (int)low.z, (int)low.w, (int)high.x, (int)high.y, (int)high.z, (int)high.w};
@@ -155,10 +161,10 @@ template <int HEIGHT>
 struct GroupTiles {
   int first, end, tiles_before, tiles_with;
   __device__ __forceinline__ GroupTiles(const ProductArgs &a, int base, int row0, int tile0) {
-    const int group = base + (threadIdx.x & 63), rows = (int)a.rows;
+    const int group = base + (threadIdx.x & 63), rows = a.rows;
     int size = 0;
     if (group < a.groups) {
-      if (a.group_sizes_bytes == 8) size = (int)max((int64_t)0, min(static_cast<const int64_t *>(a.group_sizes)[group], a.rows));
+      if (a.group_sizes_bytes == 8) size = (int)max((int64_t)0, min(static_cast<const int64_t *>(a.group_sizes)[group], (int64_t)rows));
       else size = max(0, min(static_cast<const int32_t *>(a.group_sizes)[group], rows));
     }
     const int with = lanes_below(size);
@@ -183,7 +189,7 @@ __device__ __forceinline__ RowTile grouped_tile(const ProductArgs &a, const Tile
     base += 64;
     g = GroupTiles<HEIGHT>(a, base, row, tiles);
   }
-  const int rows = (int)a.rows, behind = row, first_behind = tiles;
+  const int rows = a.rows, behind = row, first_behind = tiles;
   const int tile = tile_of(tiles + (rows - row + HEIGHT - 1) / HEIGHT);
   if (tile < 0) return {0, 0, 0};
   if (tile >= first_behind) {
@@ -220,7 +226,7 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs &a, int64_t row)
 template <int MT, int NT, bool EXACT, bool GROUPED>
 __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_kernel(const ProductArgs a) {
   extern __shared__ __align__(16) f32x4 s_part[];                // [wave][row tile][column tile][lane]
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = a.extent;
   const int p = lane >> 4, col0 = blockIdx.x * (16 * NT);
   RowTile t;
   if constexpr (GROUPED) {
@@ -228,7 +234,7 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
     if (t.end <= t.first) return;
   } else {
     t.first = (int64_t)blockIdx.y * (16 * MT);
-    t.end = min(t.first + 16 * MT, a.rows);
+    t.end = min(t.first + 16 * MT, (int64_t)a.rows);
     t.group = 0;
   }
   f32x4 acc[MT][NT];
@@ -239,7 +245,7 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
   bool none[MT];
   if (t.group >= 0) {
     const unsigned char *x[MT], *w[NT];
-    const float *xs[MT], *ws = a.w_scales + ((int64_t)t.group * a.n_blocks + col0 / kScaleBlock) * a.k_blocks;
+    const float *xs[MT], *ws = a.w_scales + ((int64_t)t.group * a.n_blocks() + col0 / kScaleBlock) * a.k_blocks();
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const int64_t row = source_row<GROUPED>(a, min(t.first + 16 * m + (lane & 15), t.end - 1));
@@ -284,7 +290,7 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
 #pragma unroll
       for (int d = 0; d < kDepth; ++d) if (b + d * waves < whole) multiply(held[d]);
     }
-    if (whole < a.k_blocks && whole % waves == wave) {
+    if (whole < a.k_blocks() && whole % waves == wave) {
       Block last;
       read(last, whole, std::true_type{});
       multiply(last);
@@ -317,9 +323,9 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
 }
 
 template <int MT, int NT, bool EXACT, bool GROUPED>
-int launch_direct(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
+int launch_direct(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
   if (row_tiles > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
-  const int waves = std::min(a.k_blocks, 16);
+  const int waves = a.extent = std::min(a.k_blocks(), 16);
   const dim3 grid((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)row_tiles);
   lutkan::plan_note("fp8_direct rows=%d columns=%d waves=%d; ", 16 * MT, 16 * NT, waves);
   hipLaunchKernelGGL((lutkan_fp8_direct_kernel<MT, NT, EXACT, GROUPED>), grid, dim3(64 * waves), waves > 1 ? (size_t)waves * MT * NT * 64 * sizeof(f32x4) : 0, s, a);
@@ -358,7 +364,7 @@ struct Tile {
 };
 
 template <int MT, int NT, int WM, int WN, int KG, int STAGES, bool EXACT, bool GROUPED, bool ASYNC>
-__global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void lutkan_fp8_tiled_kernel(const ProductArgs a, unsigned row_tiles) {
+__global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void lutkan_fp8_tiled_kernel(const ProductArgs a) {
   using T = Tile<MT, NT, WM, WN, KG, STAGES>;
   constexpr int kRows = T::kRows, kCols = T::kCols, kWaves = WM * WN, kThreads = T::kThreads, kScalesAt = T::kScalesAt, kStage = T::kStage;
   constexpr int kXCopies = kRows / 8 / kWaves, kWCopies = kCols / 8 / kWaves, kCopies = kXCopies + kWCopies;     // of 8 rows, for each wave
@@ -384,8 +390,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
   if constexpr (GROUPED) {
     t = grouped_tile<kRows>(a, tile_of);
   } else {
-    t.first = (int64_t)tile_of(row_tiles) * kRows;               // (the grid has as many work-groups as there are tiles)
-    t.end = min(t.first + kRows, a.rows);
+    t.first = (int64_t)tile_of(a.extent) * kRows;               // (the grid has as many work-groups as there are tiles)
+    t.end = min(t.first + kRows, (int64_t)a.rows);
     t.group = 0;
   }
   if (t.end <= t.first) return;
@@ -413,8 +419,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
     for (int c = 0; c < kWCopies; ++c) w_from[c] = (offset_t)((int64_t)min((wave * kWCopies + c) * 8 + (lane >> 3), a.n - 1 - col0) * a.w_stride);
     scale_from = (offset_t)(row_of(min(tid, kRows - 1)) * a.x_scales_stride * 4);
     constexpr int kColBlocks = kCols > kScaleBlock ? kCols / kScaleBlock : 1;    // (a tile of fewer columns lies in one block)
-    const float *w_scales_tile = a.w_scales + ((int64_t)t.group * a.n_blocks + col0 / kScaleBlock) * a.k_blocks;
-    const unsigned w_scale_from = (unsigned)(min(lane, a.n_blocks - 1 - col0 / kScaleBlock) * a.k_blocks) * 4;
+    const float *w_scales_tile = a.w_scales + ((int64_t)t.group * a.n_blocks() + col0 / kScaleBlock) * a.k_blocks();
+    const unsigned w_scale_from = (unsigned)(min(lane, a.n_blocks() - 1 - col0 / kScaleBlock) * a.k_blocks()) * 4;
     const int whole = a.k / kScaleBlock, own = (whole - team + KG - 1) / KG, steps = (whole + KG - 1) / KG;     // whole blocks: all, this team's, the first team's
     unsigned char *const s_team = s_tiles + team * STAGES * kStage;
     const auto block_of = [&](int step) { return step * KG + team; };
@@ -525,7 +531,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
       if (step < own) multiply(step, step + STAGES - 1 < own);
       if (step + 1 < own) put(step + 1);
     }
-    if (whole < a.k_blocks) {
+    if (whole < a.k_blocks()) {
       const bool mine = whole % KG == team;
       if (mine) put_end();                                       // (into a buffer that nobody reads since the last barrier)
       lds_barrier();
@@ -561,20 +567,21 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
 }
 
 template <int MT, int NT, int WM, int WN, int KG, int STAGES, bool EXACT, bool GROUPED, bool ASYNC>
-int launch_tiles(const ProductArgs &a, int64_t row_tiles, const char *who, hipStream_t s) {
+int launch_tiles(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
   using T = Tile<MT, NT, WM, WN, KG, STAGES>;
   static LdsCap cap;
+  a.extent = (int32_t)row_tiles;
   const auto kernel = lutkan_fp8_tiled_kernel<MT, NT, WM, WN, KG, STAGES, EXACT, GROUPED, ASYNC>;
   if (int rc = raise_lds_cap(kernel, &cap, who)) return rc;
   lutkan::plan_note("fp8_tiled rows=%d columns=%d teams=%d stages=%d%s; ", T::kRows, T::kCols, KG, STAGES, ASYNC ? " async" : "");
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * ((a.n + T::kCols - 1) / T::kCols))), dim3(T::kThreads * KG), T::kLds, s, a, (unsigned)row_tiles);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * ((a.n + T::kCols - 1) / T::kCols))), dim3(T::kThreads * KG), T::kLds, s, a);
   return check_launch(who);
 }
 
 // Rows at dword addresses, as global loads of several dwords ask for, and at offsets that the copies can hold.
 template <bool GROUPED>
 bool copies_async(const ProductArgs &a) {
-  const int64_t x_span = GROUPED ? a.x_rows : 256, most = (int64_t)1 << 32;
+  const int64_t x_span = GROUPED ? std::max(a.x_rows, 1) : 256, most = (int64_t)1 << 32;
   return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 3) == 0 &&
          a.x_stride < most / x_span && a.x_scales_stride < most / 4 / x_span && a.w_stride < most / 256;
 }
@@ -597,17 +604,17 @@ template <bool EXACT, bool GROUPED>
 int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   const int64_t groups = GROUPED ? a.groups : 1;
   const auto tiles = [&](int height) {                           // no routing has more
-    return GROUPED ? a.rows / height + std::min<int64_t>(groups + 1, a.rows) : (a.rows + height - 1) / height;
+    return GROUPED ? a.rows / height + std::min<int64_t>(groups + 1, a.rows) : ((int64_t)a.rows + height - 1) / height;
   };
   const auto likely_tiles = [&](int height) {                    // of a routing of some spread: a group's last tile is half empty
     if (!GROUPED) return (double)tiles(height);
-    const double some = (double)std::min(groups, a.rows), each = (double)a.rows / some;
+    const double some = (double)std::min<int64_t>(groups, a.rows), each = (double)a.rows / some;
     return some * std::max(1.0, each / height + (each > 1 ? 0.6 : 0.0));
   };
   if (tiles(64) * ((a.n + 63) / 64) > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   lutkan::plan_clear();
   const bool async = copies_async<GROUPED>(a);
-  const double likely_rows = (double)a.rows / (double)std::min(groups, a.rows), k_blocks = a.k_blocks;
+  const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows), k_blocks = a.k_blocks();
   const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
     return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one, all, ends, std::ceil(k_blocks / teams));
   };
@@ -646,15 +653,16 @@ int check_product(const lutkan_matmul_fp8_args *p, const char *who, ProductArgs 
   if (p->n > LUTKAN_FP8_MAX_INPUTS) return fail(LUTKAN_EUNSUPPORTED, "%s: %d outputs, at most %d", who, p->n, LUTKAN_FP8_MAX_INPUTS);
   if (!is_type(p->y_type)) return fail(LUTKAN_EINVAL, "%s: bad type", who);
   if (p->rows > 0 && (!p->x || !p->x_scales || !p->weight || !p->weight_scales || !p->y)) return fail(LUTKAN_EINVAL, "%s: null x / x_scales / weight / weight_scales / y", who);
-  const int64_t k_blocks = scale_blocks(p->k);
   if (p->y_stride < p->n) return fail(LUTKAN_ESHAPE, "%s: a row of y is longer than its stride", who);
   if (p->x_stride < 0 || p->weight_stride < 0 || p->x_scales_stride < 0 || p->weight_matrix_stride < 0) return fail(LUTKAN_ESHAPE, "%s: negative stride", who);
+  if (std::max({p->x_stride, p->weight_stride, p->x_scales_stride, p->y_stride, p->rows, p->x_rows}) > INT32_MAX)
+    return fail(LUTKAN_EUNSUPPORTED, "%s: row strides and rows of at most 2^31 - 1", who);
   *a = ProductArgs{};
   a->x = static_cast<const unsigned char *>(p->x); a->w = static_cast<const unsigned char *>(p->weight);
   a->x_scales = p->x_scales; a->w_scales = p->weight_scales; a->y = static_cast<unsigned char *>(p->y);
-  a->x_rows = p->x_rows; a->x_stride = p->x_stride; a->x_scales_stride = p->x_scales_stride;
-  a->w_stride = p->weight_stride; a->w_matrix_stride = p->weight_matrix_stride; a->y_stride = p->y_stride;
-  a->rows = p->rows; a->k = p->k; a->n = p->n; a->k_blocks = (int32_t)k_blocks; a->n_blocks = (int32_t)scale_blocks(p->n); a->y_type = p->y_type;
+  a->x_rows = (int32_t)p->x_rows; a->x_stride = (int32_t)p->x_stride; a->x_scales_stride = (int32_t)p->x_scales_stride;
+  a->w_stride = (int32_t)p->weight_stride; a->w_matrix_stride = p->weight_matrix_stride; a->y_stride = (int32_t)p->y_stride;
+  a->rows = (int32_t)p->rows; a->k = p->k; a->n = p->n; a->y_type = (int8_t)p->y_type;
   return LUTKAN_OK;
 }
 
@@ -684,6 +692,6 @@ extern "C" int lutkan_grouped_matmul_fp8(const lutkan_matmul_fp8_args *p, void *
   if (!p->row_index && p->rows != p->x_rows) return fail(LUTKAN_ESHAPE, "%s: %lld rows out, %lld in, and no row_index", who, (long long)p->rows, (long long)p->x_rows);
   if (p->row_index && p->x_rows == 0) return fail(LUTKAN_ESHAPE, "%s: row_index into no rows", who);
   a.group_sizes = p->group_sizes; a.row_index = p->row_index; a.groups = p->groups;
-  a.group_sizes_bytes = p->group_sizes_bytes; a.row_index_bytes = p->row_index_bytes;
+  a.group_sizes_bytes = (int8_t)p->group_sizes_bytes; a.row_index_bytes = (int8_t)p->row_index_bytes;
   return a.y_type == LUTKAN_F32 ? launch_product<true, true>(a, who, s) : launch_product<false, true>(a, who, s);
 }

@@ -415,6 +415,7 @@ def test_the_library_refuses_bad_arguments():
     for change in ({"codes_stride": 127}, {"scales_stride": 0}, {"residual_out_stride": 5}, {"x_stride": -128}, {"residual_stride": -1}):
         _refused(-2, norm(**change))
     _refused(-5, norm(width=32769, codes_stride=40000, scales_stride=400, residual_out_stride=40000))
+    _refused(-5, norm(x_stride=1 << 31))
     assert norm(rows=0, x=None) == 0
 
     def weights(w=4096, t=0, matrices=1, n=4, k=4, stride=4, matrix_stride=16, codes=4096, scales=4096):
@@ -436,7 +437,7 @@ def test_the_library_refuses_bad_arguments():
             _refused(-1, product(f, **change))
         for change in ({"y_stride": 7}, {"x_stride": -1}, {"weight_stride": -1}, {"x_scales_stride": -1}, {"rows": 3}):
             _refused(-2, product(f, **change))
-        for change in ({"k": (1 << 20) + 1}, {"n": (1 << 20) + 1, "y_stride": 1 << 21}):
+        for change in ({"k": (1 << 20) + 1}, {"n": (1 << 20) + 1, "y_stride": 1 << 21}, {"x_stride": 1 << 31}, {"weight_stride": 1 << 31}, {"rows": 1 << 31, "x_rows": 1 << 31}):
             _refused(-5, product(f, **change))
         assert product(f, rows=0, x_rows=0) == 0
     f = "lutkan_grouped_matmul_fp8"
@@ -444,6 +445,7 @@ def test_the_library_refuses_bad_arguments():
         _refused(-1, product(f, **change))
     for change in ({"weight_matrix_stride": -1}, {"row_index": 4096, "x_rows": 0}):
         _refused(-2, product(f, **change))
+    _refused(-5, product(f, rows=(1 << 24) + 1, x_rows=(1 << 24) + 1))
 
 
 def test_the_binding_refuses_tensors_of_the_wrong_shape_dtype_or_device():
