@@ -801,7 +801,8 @@ def lutkan_rmsnorm_fp8(x, weight, residual=None, eps: float = 1e-6, residual_out
     """Residual addition, root-mean-square norm and conversion to 8-bit floating point in one pass, on the current stream.
     x [rows, width] and residual [rows, width] float32, float16 or bfloat16, each its own; weight [width].
     Returns (codes, scales, residual_out): float8_e4m3fn [rows, width], float32 [rows, ceil(width / 128)], and x + residual in the
-    residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself."""
+    residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself.  Codes and scales, which are
+    used together, may share one allocation."""
     if residual_out is None:
         out = (_native or _native_calls()).rmsnorm_fp8(x, weight, residual, eps)
         if out is not None:

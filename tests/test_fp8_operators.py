@@ -495,3 +495,63 @@ def test_the_binding_refuses_operands_that_do_not_fit():
     refused("without a residual", lk.lutkan_rmsnorm_fp8, v, torch.ones(130, device=DEV), residual_out=v)
     refused("residual_out must", lk.lutkan_rmsnorm_fp8, v, torch.ones(130, device=DEV), residual=v, residual_out=v.half())
     refused("EUNSUPPORTED|\\[-5\\]", lk.lutkan_rmsnorm_fp8, torch.zeros(1, 40000, device=DEV), torch.ones(40000, device=DEV))
+
+
+# ---------------------------------------------------------------- the operators together, and their code
+@gpu
+@pytest.mark.parametrize("tokens", [1, 37, 600])
+def test_expert_block(tokens):
+    """The block's output from its own codes and routing: the experts' products in 64 bits, the table layer's kernel on them, and the
+    weighted sum over a token's experts.  Bound: the products' as above; the layer is Lipschitz between its table's points (its steps
+    at the knots are small and rare), and bf16 rounds the output: 2 % of the output's norm covers all of it."""
+    from paper_2601_03332_amd.expert_block import ExpertBlock
+    rng = np.random.default_rng(tokens)
+    width, inner, experts, top = 200, 48, 5, 2
+    knots = (-4.0 + (np.arange(15) - 3) * 1.0).astype(np.float32)
+    art = lk.lutkan_compile(inner, width, 8, 3, knots, (rng.standard_normal((inner, width, 11)) / 7).astype(np.float32), 32, lk.ASYM_UINT8, lk.CLOSED, lk.CLIP_X)
+    layer = art.to_device(DEV)
+
+    def normal(*shape):
+        return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(DEV)
+    norm = 1 + 0.1 * normal(width)
+    block = ExpertBlock(norm, normal(experts, width) / width ** 0.5, normal(experts, inner, width) / width ** 0.5, layer, top)
+    x, residual = normal(tokens, width).bfloat16(), normal(tokens, width)
+    y, res = block(x, residual)
+    assert torch.equal(res, x.float() + residual) and y.dtype == torch.bfloat16
+    codes, scales, _ = lk.lutkan_rmsnorm_fp8(x, norm, residual=residual)
+    p, expert = torch.softmax(lk.lutkan_matmul_fp8(codes, scales, *block.router), 1).topk(top, 1)
+    codes, scales, w, ws = codes.cpu(), scales.cpu(), block.experts[0].cpu(), block.experts[1].cpu()
+    out = np.zeros((tokens, width))
+    for place in range(top):
+        z = np.zeros((tokens, inner), np.float32)
+        for e in range(experts):
+            at = torch.where(expert[:, place].cpu() == e)[0]
+            if at.numel():
+                z[at.numpy()] = product_reference(codes.view(torch.uint8)[at].view(F8), scales[at], w[e], ws[e])[0]
+        out += p[:, place, None].cpu().numpy() * lk.lutkan_forward(layer, torch.from_numpy(z).to(DEV)).cpu().numpy()
+    assert np.linalg.norm(y.float().cpu().numpy() - out) <= 0.02 * np.linalg.norm(out)
+
+
+def test_m0_is_only_touched_by_the_lds_copies_in_the_products_kernels(tmp_path):
+    """The copies into LDS write M0 inside inline-asm blocks and declare it clobbered, which is sound while the compiler keeps nothing in
+    M0 there: in the generated code every mention of it lies in such a block."""
+    import os
+    import re
+    import subprocess
+    from paper_2601_03332_amd import build as lib_build
+    out = tmp_path / "matmul.s"
+    cmd = [os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")] + lib_build.HIPCC_FLAGS + ["-I", os.path.join(lib_build.ROOT, "include"), "-I", lib_build.CSRC, "-x", "hip",
+                                                                                      "--cuda-device-only", "-S", os.path.join(lib_build.CSRC, "lutkan_fp8_matmul.hip"), "-o", str(out)]
+    subprocess.run(cmd, check=True, capture_output=True)
+    kernels, inside_asm, current = 0, False, None
+    for line in open(out):
+        text = line.strip()
+        if re.match(r"_Z\S*fp8_tiled_kernel\S*:", text):
+            current, kernels = text.split(":")[0], kernels + 1
+        elif text.startswith(".Lfunc_end"):
+            current = None
+        elif text.startswith(";;#ASM"):
+            inside_asm = text.startswith(";;#ASMSTART")
+        elif current and not text.startswith(";") and re.search(r"\bm0\b", text.split(";")[0]):
+            assert inside_asm, f"compiler-generated use of m0 in {current}: {text}"
+    assert kernels >= 16
