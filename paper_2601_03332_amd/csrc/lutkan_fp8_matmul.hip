@@ -581,7 +581,7 @@ int launch_tiles(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t 
 // Rows at dword addresses, as global loads of several dwords ask for, and at offsets that the copies can hold.
 template <bool GROUPED>
 bool copies_async(const ProductArgs &a) {
-  const int64_t x_span = GROUPED ? std::max(a.x_rows, 1) : 256, most = (int64_t)1 << 32;
+  const int64_t x_span = GROUPED ? std::max(a.x_rows, 1) : 256, most = ((int64_t)1 << 32) - kScaleBlock;     // (a block's columns beside the row's offset)
   return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 3) == 0 &&
          a.x_stride < most / x_span && a.x_scales_stride < most / 4 / x_span && a.w_stride < most / 256;
 }
