@@ -57,12 +57,32 @@ __device__ u32x4 piece_at_end(const unsigned char *row, int k0, int k) {
   return __builtin_bit_cast(u32x4, codes);
 }
 
-// The 32 codes of a block that lane-sixteenth `p` takes of a row.
-template <bool END>
-__device__ __forceinline__ i32x8 block_of_row(const unsigned char *row, int k0, int p, int k) {
-  if constexpr (END) return fragment(piece_at_end(row, k0 + 16 * p, k), piece_at_end(row, k0 + 64 + 16 * p, k));
-  else return fragment(load_any<u32x4>(row + k0 + 16 * p), load_any<u32x4>(row + k0 + 64 + 16 * p));
-}
+// Sixteen codes of a row as they are read.  ALIGNED: the row lies at a dword address.  Otherwise the five dwords that hold a byte of
+// them (the fifth is the fourth again where the codes lie at one after all), moved into place when they are used, as loads of 16 bytes
+// that are not dword-aligned are slower: 70 rows of 4551 -> 240 14.1 -> 8.8 us, 143 of 4395 -> 1504 25 -> 16.
+template <bool ALIGNED>
+struct Piece {
+  u32x4 codes;
+  __device__ __forceinline__ void read(const unsigned char *p) { codes = load_any<u32x4>(p); }
+  __device__ __forceinline__ u32x4 get(unsigned) const { return codes; }
+};
+template <>
+struct Piece<false> {
+  u32x4 first;
+  unsigned last;
+  __device__ __forceinline__ void read(const unsigned char *p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    first = load_any<u32x4>(reinterpret_cast<const unsigned *>(at & ~(uintptr_t)3));
+    last = *reinterpret_cast<const unsigned *>((at + 15) & ~(uintptr_t)3);
+  }
+  // `at`: the low bits of the address they were read from.
+  __device__ __forceinline__ u32x4 get(unsigned at) const {
+    return u32x4{__builtin_amdgcn_alignbyte(first.y, first.x, at), __builtin_amdgcn_alignbyte(first.z, first.y, at), __builtin_amdgcn_alignbyte(first.w, first.z, at),
+                 __builtin_amdgcn_alignbyte(last, first.w, at)};
+  }
+};
+
+__device__ __forceinline__ unsigned low_bits(const void *p) { return (unsigned)reinterpret_cast<uintptr_t>(p); }
 
 // A lane's 32 codes of a block as the instruction takes them: EXACT = false as they are, true as bf16.
 template <bool EXACT>
@@ -223,7 +243,7 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs &a, int64_t row)
 
 // A work-group computes 16 MT rows x 16 NT columns from global memory straight into registers; its waves take the blocks of k in turn,
 // and their sums meet in LDS in the waves' order.
-template <int MT, int NT, bool EXACT, bool GROUPED>
+template <int MT, int NT, bool EXACT, bool GROUPED, bool ALIGNED>
 __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_kernel(const ProductArgs a) {
   extern __shared__ __align__(16) f32x4 s_part[];                // [wave][row tile][column tile][lane]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = a.extent;
@@ -257,43 +277,62 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
     for (int n = 0; n < NT; ++n) w[n] = a.w + t.group * a.w_matrix_stride + (int64_t)min(col0 + 16 * n + (lane & 15), a.n - 1) * a.w_stride;
     // Codes and scales of a block, and its products: kDepth blocks are read before the first is multiplied.
     constexpr int kDepth = MT * NT == 1 ? 4 : MT * NT == 2 ? 2 : 1;
-    struct Block { i32x8 w[NT], x[MT]; float scale[MT]; };
-    const auto read = [&](Block &to, int b, auto at_end) {
+    struct Block { Piece<ALIGNED> w[NT][2], x[MT][2]; float scale[MT]; };
+    const auto read_scales = [&](float (&scale)[MT], int b) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) to.w[n] = block_of_row<decltype(at_end)::value>(w[n], b * kScaleBlock, p, a.k);
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        to.x[m] = block_of_row<decltype(at_end)::value>(x[m], b * kScaleBlock, p, a.k);
-        to.scale[m] = xs[m][b] * ws[b];
-      }
+      for (int m = 0; m < MT; ++m) scale[m] = xs[m][b] * ws[b];
     };
-    const auto multiply = [&](const Block &of) {
+    const auto read = [&](Block &to, int b) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) to.w[n][h].read(w[n] + b * kScaleBlock + 64 * h + 16 * p);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) to.x[m][h].read(x[m] + b * kScaleBlock + 64 * h + 16 * p);
+      }
+      read_scales(to.scale, b);
+    };
+    const auto multiply = [&](const i32x8 (&wc)[NT], const i32x8 (&xc)[MT], const float (&scale)[MT]) {
       Operand<EXACT> wf[NT], xf;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) wf[n].set(of.w[n]);
+      for (int n = 0; n < NT; ++n) wf[n].set(wc[n]);
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        xf.set(of.x[m]);
+        xf.set(xc[m]);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const f32x4 v = block_product(wf[n], xf);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[m][n][e] = fmaf(of.scale[m], v[e], acc[m][n][e]);
+          for (int e = 0; e < 4; ++e) acc[m][n][e] = fmaf(scale[m], v[e], acc[m][n][e]);
         }
       }
+    };
+    const auto multiply_block = [&](const Block &of) {
+      i32x8 wc[NT], xc[MT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) wc[n] = fragment(of.w[n][0].get(low_bits(w[n])), of.w[n][1].get(low_bits(w[n])));
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xc[m] = fragment(of.x[m][0].get(low_bits(x[m])), of.x[m][1].get(low_bits(x[m])));
+      multiply(wc, xc, of.scale);
     };
     const int whole = a.k / kScaleBlock;
     for (int b = wave; b < whole; b += waves * kDepth) {
       Block held[kDepth];
 #pragma unroll
-      for (int d = 0; d < kDepth; ++d) if (b + d * waves < whole) read(held[d], b + d * waves, std::false_type{});
+      for (int d = 0; d < kDepth; ++d) if (b + d * waves < whole) read(held[d], b + d * waves);
 #pragma unroll
-      for (int d = 0; d < kDepth; ++d) if (b + d * waves < whole) multiply(held[d]);
+      for (int d = 0; d < kDepth; ++d) if (b + d * waves < whole) multiply_block(held[d]);
     }
-    if (whole < a.k_blocks() && whole % waves == wave) {
-      Block last;
-      read(last, whole, std::true_type{});
-      multiply(last);
+    if (whole < a.k_blocks() && whole % waves == wave) {         // the last block, not whole
+      i32x8 wc[NT], xc[MT];
+      float scale[MT];
+      const int k0 = whole * kScaleBlock + 16 * p;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) wc[n] = fragment(piece_at_end(w[n], k0, a.k), piece_at_end(w[n], k0 + 64, a.k));
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xc[m] = fragment(piece_at_end(x[m], k0, a.k), piece_at_end(x[m], k0 + 64, a.k));
+      read_scales(scale, whole);
+      multiply(wc, xc, scale);
     }
   } else {
 #pragma unroll
@@ -323,12 +362,13 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
 }
 
 template <int MT, int NT, bool EXACT, bool GROUPED>
-int launch_direct(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
+int launch_direct(ProductArgs a, int64_t row_tiles, bool aligned, const char *who, hipStream_t s) {
   if (row_tiles > 65535) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
   const int waves = a.extent = std::min(a.k_blocks(), 16);
   const dim3 grid((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)row_tiles);
   lutkan::plan_note("fp8_direct rows=%d columns=%d waves=%d; ", 16 * MT, 16 * NT, waves);
-  hipLaunchKernelGGL((lutkan_fp8_direct_kernel<MT, NT, EXACT, GROUPED>), grid, dim3(64 * waves), waves > 1 ? (size_t)waves * MT * NT * 64 * sizeof(f32x4) : 0, s, a);
+  const auto kernel = aligned ? lutkan_fp8_direct_kernel<MT, NT, EXACT, GROUPED, true> : lutkan_fp8_direct_kernel<MT, NT, EXACT, GROUPED, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), waves > 1 ? (size_t)waves * MT * NT * 64 * sizeof(f32x4) : 0, s, a);
   return check_launch(who);
 }
 
@@ -425,7 +465,12 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
     unsigned char *const s_team = s_tiles + team * STAGES * kStage;
     const auto block_of = [&](int step) { return step * KG + team; };
     const auto stage = [&](int step) { return s_team + (step & (STAGES - 1)) * kStage; };
-    u32x4 held[ASYNC ? 1 : kCopies];
+    Piece<false> held[ASYNC ? 1 : kCopies];                      // (without ASYNC: rows at any address)
+    float held_scale, held_w_scale;
+    const auto ask_scales = [&](int64_t b) {
+      held_scale = load_any<float>(reinterpret_cast<const unsigned char *>(scales_tile + b) + scale_from);
+      held_w_scale = load_any<float>(reinterpret_cast<const unsigned char *>(w_scales_tile + b) + w_scale_from);
+    };
     // The pieces of this team's block of a step are asked for, copy by copy, and put into their buffer: at once where they go straight
     // there, else by put().
     const auto ask = [&](int step, int c) {
@@ -438,32 +483,34 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
         if (c == 0 && wave < kRows / 64) copy4_global_to_lds_at(scales_tile + b, scale_from, stage(step) + kScalesAt + wave * 256);
         if (c == 0 && wave == kWaves - 1 && lane < kColBlocks) copy4_global_to_lds_at(w_scales_tile + b, w_scale_from, stage(step) + kScalesAt + kRows * 4);
       } else {
-        held[c] = load_any<u32x4>((of_x ? x_tile + x_from[c] : w_tile + w_from[cw]) + (b * kScaleBlock + piece_at[c & 1]));
+        if (c == 0) ask_scales(b);
+        held[c].read((of_x ? x_tile + x_from[c] : w_tile + w_from[cw]) + (b * kScaleBlock + piece_at[c & 1]));
       }
     };
-    const auto put_scales = [&](int step, int b) {
+    const auto put_scales = [&](int step) {
       float *to = reinterpret_cast<float *>(stage(step) + kScalesAt);
-      if (tid < kRows) to[tid] = load_any<float>(reinterpret_cast<const unsigned char *>(scales_tile + b) + scale_from);
-      if (tid < kColBlocks) to[kRows + tid] = load_any<float>(reinterpret_cast<const unsigned char *>(w_scales_tile + b) + w_scale_from);
+      if (tid < kRows) to[tid] = held_scale;
+      if (tid < kColBlocks) to[kRows + tid] = held_w_scale;
     };
     const auto put = [&](int step) {
       if constexpr (!ASYNC) {
         unsigned char *to = stage(step) + lane * 16;
 #pragma unroll
-        for (int c = 0; c < kXCopies; ++c) *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = held[c];
+        for (int c = 0; c < kXCopies; ++c) *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = held[c].get(low_bits(x_tile + x_from[c]));
 #pragma unroll
-        for (int c = 0; c < kWCopies; ++c) *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = held[kXCopies + c];
-        put_scales(step, block_of(step));
+        for (int c = 0; c < kWCopies; ++c) *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = held[kXCopies + c].get(low_bits(w_tile + w_from[c]));
+        put_scales(step);
       }
     };
     // The last block, if it is not whole: this team's step `own`.
     const auto put_end = [&]() {
+      ask_scales(whole);
       unsigned char *to = stage(own) + lane * 16;
       for (int c = 0; c < kXCopies; ++c)
         *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = piece_at_end(x_tile + x_from[c], whole * kScaleBlock + piece_at[c & 1], a.k);
       for (int c = 0; c < kWCopies; ++c)
         *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = piece_at_end(w_tile + w_from[c], whole * kScaleBlock + piece_at[c & 1], a.k);
-      put_scales(own, whole);
+      put_scales(own);
     };
     const int at_row = lane & 15, low = at_row * kScaleBlock + piece_place(at_row, p) * 16, high_half = at_row * kScaleBlock + piece_place(at_row, p + 4) * 16;
     // One block: the products in a fixed order, each added two products after it was begun; a row subtile's codes are read while the one
@@ -567,7 +614,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
 }
 
 template <int MT, int NT, int WM, int WN, int KG, int STAGES, bool EXACT, bool GROUPED, bool ASYNC>
-int launch_tiles(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
+int launch_tiles_as(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
   using T = Tile<MT, NT, WM, WN, KG, STAGES>;
   static LdsCap cap;
   a.extent = (int32_t)row_tiles;
@@ -578,12 +625,18 @@ int launch_tiles(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t 
   return check_launch(who);
 }
 
-// Rows at dword addresses, as global loads of several dwords ask for, and at offsets that the copies can hold.
+template <int MT, int NT, int WM, int WN, int KG, bool EXACT, bool GROUPED>
+int launch_tiles(const ProductArgs &a, int64_t row_tiles, bool async, const char *who, hipStream_t s) {
+  return async ? launch_tiles_as<MT, NT, WM, WN, KG, 2, EXACT, GROUPED, true>(a, row_tiles, who, s) : launch_tiles_as<MT, NT, WM, WN, KG, 2, EXACT, GROUPED, false>(a, row_tiles, who, s);
+}
+
+bool rows_aligned(const ProductArgs &a) {                        // every row at a dword address
+  return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 3) == 0;
+}
 template <bool GROUPED>
-bool copies_async(const ProductArgs &a) {
-  const int64_t x_span = GROUPED ? std::max(a.x_rows, 1) : 256, most = ((int64_t)1 << 32) - kScaleBlock;     // (a block's columns beside the row's offset)
-  return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.x_stride | (uintptr_t)a.w_stride | (uintptr_t)a.w_matrix_stride) & 3) == 0 &&
-         a.x_stride < most / x_span && a.x_scales_stride < most / 4 / x_span && a.w_stride < most / 256;
+bool copies_fit(const ProductArgs &a) {                          // the rows' offsets, as the copies hold them
+  const int64_t x_span = GROUPED ? std::max(a.x_rows, 1) : 256, most = ((int64_t)1 << 32) - kScaleBlock;     // (a block's columns beside them)
+  return a.x_stride < most / x_span && a.x_scales_stride < most / 4 / x_span && a.w_stride < most / 256;
 }
 
 // What a launch takes beyond an empty one, in us, for the kernels' choice; fitted to times from 1 to 8192 rows, 128 to 8192 inputs and
@@ -613,7 +666,7 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   };
   if (tiles(64) * ((a.n + 63) / 64) > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   lutkan::plan_clear();
-  const bool async = copies_async<GROUPED>(a);
+  const bool aligned = rows_aligned(a), async = aligned && copies_fit<GROUPED>(a);
   const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows), k_blocks = a.k_blocks();
   const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
     return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one, all, ends, std::ceil(k_blocks / teams));
@@ -628,22 +681,24 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   price[kTiled128x2] = EXACT ? tiled(128, 1, 1.75, 1.75, 5, 2) : tiled(128, 1, 1.0, 1.0, 5, 2);
   price[kTiled128] = EXACT ? tiled(128, 2, 1.3, 1.9, 2, 1) : tiled(128, 2, 0.65, 1.08, 2, 1);
   price[kTiled256] = EXACT ? HUGE_VAL : tiled(256, 1, 1.6, 1.6, 6, 1);
-  if (!async)                                                    // (through registers: one kernel of the tiled ones)
-    for (int k : {kTiled64x4, kTiled64x2, kTiled128x2, kTiled256}) price[k] = HUGE_VAL;
+  if (!async) {                                                  // through registers, where a step waits longer; the largest tile's sums leave none
+    price[kTiled64x4] *= 2, price[kTiled64x2] *= 2;
+    price[kTiled128x2] *= 1.5, price[kTiled128] *= 1.5;
+    price[kTiled256] = HUGE_VAL;
+  }
   if (tiles(16) > 65535) price[kDirect16x16] = price[kDirect16x32] = HUGE_VAL;
   if (tiles(32) > 65535) price[kDirect32x32] = HUGE_VAL;
   const int pick = (int)(std::min_element(price, price + kKernels) - price);
   switch (pick) {
-    case kDirect16x16: return launch_direct<1, 1, EXACT, GROUPED>(a, tiles(16), who, s);
-    case kDirect16x32: return launch_direct<1, 2, EXACT, GROUPED>(a, tiles(16), who, s);
-    case kDirect32x32: return launch_direct<2, 2, EXACT, GROUPED>(a, tiles(32), who, s);
-    case kTiled64x4: return launch_tiles<2, 2, 2, 2, 4, 2, EXACT, GROUPED, true>(a, tiles(64), who, s);
-    case kTiled64x2: return launch_tiles<2, 2, 2, 2, 2, 2, EXACT, GROUPED, true>(a, tiles(64), who, s);
-    case kTiled128x2: return launch_tiles<4, 4, 2, 2, 2, 2, EXACT, GROUPED, true>(a, tiles(128), who, s);
-    case kTiled256: if constexpr (!EXACT) return launch_tiles<8, 4, 2, 4, 1, 2, EXACT, GROUPED, true>(a, tiles(256), who, s);
-    default: break;
+    case kDirect16x16: return launch_direct<1, 1, EXACT, GROUPED>(a, tiles(16), aligned, who, s);
+    case kDirect16x32: return launch_direct<1, 2, EXACT, GROUPED>(a, tiles(16), aligned, who, s);
+    case kDirect32x32: return launch_direct<2, 2, EXACT, GROUPED>(a, tiles(32), aligned, who, s);
+    case kTiled64x4: return launch_tiles<2, 2, 2, 2, 4, EXACT, GROUPED>(a, tiles(64), async, who, s);
+    case kTiled64x2: return launch_tiles<2, 2, 2, 2, 2, EXACT, GROUPED>(a, tiles(64), async, who, s);
+    case kTiled128x2: return launch_tiles<4, 4, 2, 2, 2, EXACT, GROUPED>(a, tiles(128), async, who, s);
+    case kTiled256: if constexpr (!EXACT) return launch_tiles_as<8, 4, 2, 4, 1, 2, EXACT, GROUPED, true>(a, tiles(256), who, s);
+    default: return launch_tiles<4, 4, 2, 2, 1, EXACT, GROUPED>(a, tiles(128), async, who, s);
   }
-  return async ? launch_tiles<4, 4, 2, 2, 1, 2, EXACT, GROUPED, true>(a, tiles(128), who, s) : launch_tiles<4, 4, 2, 2, 1, 2, EXACT, GROUPED, false>(a, tiles(128), who, s);
 }
 
 int check_product(const lutkan_matmul_fp8_args *p, const char *who, ProductArgs *a) {
