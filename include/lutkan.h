@@ -74,7 +74,7 @@ const char *lutkan_version(void);
  * np=16 split=1 pipe=3; " (base_product cuts the base rows into pieces in a launch of its own) or, for a B-spline layer on the
  * matrix cores, "bspline_matrix np=1 split=2 slots=8; sum; " (slots: up to 8, 12 or 16 coefficient rows per input; model_forward: the clauses of all its layers), or, for a product in 8 bits,
  * "fp8_direct rows=16 columns=16 waves=8; " (a tile straight from memory, waves along the inputs) or "fp8_tiled rows=128 columns=128
- * teams=2 stages=2 async; " (tiles through LDS; teams of waves along the inputs, buffers, copies without registers).  Thread-local, overwritten by the next forward call, never null. */
+ * teams=2 async; " (tiles through LDS; teams of waves along the inputs, copies without registers).  Thread-local, overwritten by the next forward call, never null. */
 const char *lutkan_last_plan(void);
 
 /* ------------------------------------------------------------------------------------------------

@@ -374,7 +374,7 @@ int launch_direct(ProductArgs a, int64_t row_tiles, bool aligned, const char *wh
 
 // A tile of 16 MT WM rows x 16 NT WN columns for a work-group of KG teams of WM x WN waves, each wave 16 MT rows x 16 NT columns of it.
 // The teams take the blocks of k in turn; their sums meet in LDS in the teams' order.  A team's blocks (both operands' codes and their
-// scales) go through LDS, in STAGES buffers: while a block is multiplied the next STAGES - 1 are on their way.  A row's eight 16-byte pieces lie in an order that depends on the row (piece_place), so that the 16 rows that a read of 16 lanes takes
+// scales) go through LDS, in two buffers: while a block is multiplied the next is on its way.  A row's eight 16-byte pieces lie in an order that depends on the row (piece_place), so that the 16 rows that a read of 16 lanes takes
 // lie in different banks (no conflict counted).
 //   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and
 //   offsets that fit 32 bits.  Otherwise, and for a last block that is not whole, through registers.
@@ -386,31 +386,24 @@ __device__ __forceinline__ void copy4_global_to_lds_at(const void *uniform_base,
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(lane_byte_offset), "s"(uniform_base) : "m0", "memory");
 }
 
-// Waits until at most N of the wave's vector memory loads are outstanding (they end in the order in which they began).
-template <int N>
-__device__ __forceinline__ void wait_vector_loads() {
-  static_assert(N < 64, "a six-bit counter");
-  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
-}
-
 // The sizes of a tile, its buffers and its team.
-template <int MT, int NT, int WM, int WN, int KG, int STAGES>
+template <int MT, int NT, int WM, int WN, int KG>
 struct Tile {
   static constexpr int kRows = 16 * MT * WM, kCols = 16 * NT * WN, kThreads = 64 * WM * WN;
   static constexpr int kScalesAt = (kRows + kCols) * kScaleBlock, kStage = kScalesAt + (kRows + 4) * 4;      // codes, scales of the rows, of the columns' blocks
   static constexpr int kParts = KG > 1 ? (KG - 1) * kRows * kCols * 4 : 0;       // the sums of all teams but the one that adds them up
-  static constexpr int kLds = KG * STAGES * kStage > kParts ? KG * STAGES * kStage : kParts;
+  static constexpr int kLds = KG * 2 * kStage > kParts ? KG * 2 * kStage : kParts;
   static_assert(kLds <= lutkan::kLdsPerWorkGroup && kStage % 16 == 0, "LDS");
 };
 
-template <int MT, int NT, int WM, int WN, int KG, int STAGES, bool EXACT, bool GROUPED, bool ASYNC>
+template <int MT, int NT, int WM, int WN, int KG, bool EXACT, bool GROUPED, bool ASYNC>
 __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void lutkan_fp8_tiled_kernel(const ProductArgs a) {
-  using T = Tile<MT, NT, WM, WN, KG, STAGES>;
+  using T = Tile<MT, NT, WM, WN, KG>;
   constexpr int kRows = T::kRows, kCols = T::kCols, kWaves = WM * WN, kThreads = T::kThreads, kScalesAt = T::kScalesAt, kStage = T::kStage;
   constexpr int kXCopies = kRows / 8 / kWaves, kWCopies = kCols / 8 / kWaves, kCopies = kXCopies + kWCopies;     // of 8 rows, for each wave
   static_assert(kXCopies * 8 * kWaves == kRows && kWCopies * 8 * kWaves == kCols && kXCopies % 2 == 0 && kWCopies % 2 == 0, "copies in pairs");
-  static_assert(kThreads >= kRows && kScaleBlock % (16 * NT) == 0 && (STAGES & (STAGES - 1)) == 0 && (ASYNC || STAGES == 2), "tile");
-  extern __shared__ __align__(16) unsigned char s_tiles[];       // [team][stage][rows of x, rows of the weight][128], scales
+  static_assert(kThreads >= kRows && kScaleBlock % (16 * NT) == 0, "tile");
+  extern __shared__ __align__(16) unsigned char s_tiles[];       // [team][buffer][rows of x, rows of the weight][128], scales
   const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave_of_all / kWaves;
   const int wave = wave_of_all % kWaves, tid = wave * 64 + lane, wm = wave / WN, wn = wave % WN, p = lane >> 4;
   // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, and in a run eight row tiles share a column
@@ -462,9 +455,9 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
     const float *w_scales_tile = a.w_scales + ((int64_t)t.group * a.n_blocks() + col0 / kScaleBlock) * a.k_blocks();
     const unsigned w_scale_from = (unsigned)(min(lane, a.n_blocks() - 1 - col0 / kScaleBlock) * a.k_blocks()) * 4;
     const int whole = a.k / kScaleBlock, own = (whole - team + KG - 1) / KG, steps = (whole + KG - 1) / KG;     // whole blocks: all, this team's, the first team's
-    unsigned char *const s_team = s_tiles + team * STAGES * kStage;
+    unsigned char *const s_team = s_tiles + team * 2 * kStage;
     const auto block_of = [&](int step) { return step * KG + team; };
-    const auto stage = [&](int step) { return s_team + (step & (STAGES - 1)) * kStage; };
+    const auto stage = [&](int step) { return s_team + (step & 1) * kStage; };
     Piece<false> held[ASYNC ? 1 : kCopies];                      // (without ASYNC: rows at any address)
     float held_scale, held_w_scale;
     const auto ask_scales = [&](int64_t b) {
@@ -515,7 +508,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
     const int at_row = lane & 15, low = at_row * kScaleBlock + piece_place(at_row, p) * 16, high_half = at_row * kScaleBlock + piece_place(at_row, p + 4) * 16;
     // One block: the products in a fixed order, each added two products after it was begun; a row subtile's codes are read while the one
     // before it is multiplied.
-    const auto multiply = [&](int step, bool ask_more) {
+    const auto multiply = [&](int step, bool ask_next) {
       const unsigned char *xt = stage(step) + (wm * 16 * MT) * kScaleBlock;
       const unsigned char *wt = stage(step) + (kRows + wn * 16 * NT) * kScaleBlock;
       const float *scales = reinterpret_cast<const float *>(stage(step) + kScalesAt) + wm * 16 * MT + at_row;
@@ -552,7 +545,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
           v[i % (kAhead + 1)] = block_product(wf[n], xf);
           __builtin_amdgcn_sched_barrier(0);
           // Copies in between: a wave waits for its turn with each, and all at once would keep it from its products.
-          if (i % kEvery == kEvery - 1 && i / kEvery < kCopies && ask_more) ask(step + STAGES - 1, i / kEvery);
+          if (i % kEvery == kEvery - 1 && i / kEvery < kCopies && ask_next) ask(step + 1, i / kEvery);
         }
         if (i >= kAhead) {
           const int of = i - kAhead;
@@ -563,19 +556,15 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
         __builtin_amdgcn_sched_barrier(0);
       }
     };
+    if (own > 0) {
 #pragma unroll
-    for (int step = 0; step < STAGES - 1; ++step)
-      if (step < own)
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) ask(step, c);
-    if (own > 0) put(0);
+      for (int c = 0; c < kCopies; ++c) ask(0, c);
+      put(0);
+    }
     for (int step = 0; step < steps; ++step) {
-      // The block is there when no more than the copies of the blocks behind it are outstanding (a wave that also copies scales waits
-      // for a few more than it has to).
-      if (step + STAGES - 1 <= own) wait_vector_loads<(STAGES - 2) * kCopies>();
-      else wait_vector_loads<0>();
-      lds_barrier();                                             // ... every wave's part of it, and nobody reads the buffer of the block before it any more
-      if (step < own) multiply(step, step + STAGES - 1 < own);
+      wait_all_vector_loads();
+      lds_barrier();                                             // the block is there, and nobody reads the buffer of the one before it any more
+      if (step < own) multiply(step, step + 1 < own);
       if (step + 1 < own) put(step + 1);
     }
     if (whole < a.k_blocks()) {
@@ -613,21 +602,21 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
   }
 }
 
-template <int MT, int NT, int WM, int WN, int KG, int STAGES, bool EXACT, bool GROUPED, bool ASYNC>
+template <int MT, int NT, int WM, int WN, int KG, bool EXACT, bool GROUPED, bool ASYNC>
 int launch_tiles_as(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
-  using T = Tile<MT, NT, WM, WN, KG, STAGES>;
+  using T = Tile<MT, NT, WM, WN, KG>;
   static LdsCap cap;
   a.extent = (int32_t)row_tiles;
-  const auto kernel = lutkan_fp8_tiled_kernel<MT, NT, WM, WN, KG, STAGES, EXACT, GROUPED, ASYNC>;
+  const auto kernel = lutkan_fp8_tiled_kernel<MT, NT, WM, WN, KG, EXACT, GROUPED, ASYNC>;
   if (int rc = raise_lds_cap(kernel, &cap, who)) return rc;
-  lutkan::plan_note("fp8_tiled rows=%d columns=%d teams=%d stages=%d%s; ", T::kRows, T::kCols, KG, STAGES, ASYNC ? " async" : "");
+  lutkan::plan_note("fp8_tiled rows=%d columns=%d teams=%d%s; ", T::kRows, T::kCols, KG, ASYNC ? " async" : "");
   hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * ((a.n + T::kCols - 1) / T::kCols))), dim3(T::kThreads * KG), T::kLds, s, a);
   return check_launch(who);
 }
 
 template <int MT, int NT, int WM, int WN, int KG, bool EXACT, bool GROUPED>
 int launch_tiles(const ProductArgs &a, int64_t row_tiles, bool async, const char *who, hipStream_t s) {
-  return async ? launch_tiles_as<MT, NT, WM, WN, KG, 2, EXACT, GROUPED, true>(a, row_tiles, who, s) : launch_tiles_as<MT, NT, WM, WN, KG, 2, EXACT, GROUPED, false>(a, row_tiles, who, s);
+  return async ? launch_tiles_as<MT, NT, WM, WN, KG, EXACT, GROUPED, true>(a, row_tiles, who, s) : launch_tiles_as<MT, NT, WM, WN, KG, EXACT, GROUPED, false>(a, row_tiles, who, s);
 }
 
 bool rows_aligned(const ProductArgs &a) {                        // every row at a dword address
@@ -643,12 +632,14 @@ bool copies_fit(const ProductArgs &a) {                          // the rows' of
 // 256 to 8192 outputs (within a fifth of them where two kernels come near each other).
 //   direct   what its work-groups read, each its own: 9 MB/us over the whole GPU
 //   tiled    rounds of as many tiles as fit the compute units, a tile's steps over k: `one` where there is one to a compute unit, `all` where
-//            there are `slots`, and `ends` before and behind the steps
+//            there are `slots`, and `ends` before and behind the steps.  Where the number of tiles is a guess (groups) and two fit a compute
+//            unit, a round that is begun counts by its part.
 inline double direct_price(double row_tiles, double rows_of_tile, int columns, const ProductArgs &a) {
   const double work_groups = row_tiles * ((a.n + columns - 1) / columns);
   return work_groups * (rows_of_tile + columns) * a.k / (9e6 * std::min(1.0, work_groups / 256));
 }
-inline double tiled_price(double tiles, int slots, double one, double all, double ends, double steps) {
+inline double tiled_price(double tiles, int slots, double one, double all, double ends, double steps, bool guess) {
+  if (guess && slots > 1 && tiles > 256) return std::max(1.0, tiles / (256 * slots)) * (steps * all + ends);
   const double full = std::floor(tiles / (256 * slots)), rest = tiles - full * 256 * slots;
   return full * (steps * all + ends) + (rest > 0 ? steps * (rest <= 256 ? one : all) + ends : 0);
 }
@@ -667,9 +658,10 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   if (tiles(64) * ((a.n + 63) / 64) > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   lutkan::plan_clear();
   const bool aligned = rows_aligned(a), async = aligned && copies_fit<GROUPED>(a);
-  const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows), k_blocks = a.k_blocks();
+  const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows);
+  const double end_block = a.k % kScaleBlock ? 2.5 : 0;          // (read, put and multiplied behind the others)
   const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
-    return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one, all, ends, std::ceil(k_blocks / teams));
+    return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one, all, ends + end_block, std::ceil(a.k / kScaleBlock / (double)teams), GROUPED);
   };
   enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kKernels };
   double price[kKernels];
@@ -681,6 +673,8 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   price[kTiled128x2] = EXACT ? tiled(128, 1, 1.75, 1.75, 5, 2) : tiled(128, 1, 1.0, 1.0, 5, 2);
   price[kTiled128] = EXACT ? tiled(128, 2, 1.3, 1.9, 2, 1) : tiled(128, 2, 0.65, 1.08, 2, 1);
   price[kTiled256] = EXACT ? HUGE_VAL : tiled(256, 1, 1.6, 1.6, 6, 1);
+  if (!aligned)                                                  // (five dwords for every four)
+    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.6;
   if (!async) {                                                  // through registers, where a step waits longer; the largest tile's sums leave none
     price[kTiled64x4] *= 2, price[kTiled64x2] *= 2;
     price[kTiled128x2] *= 1.5, price[kTiled128] *= 1.5;
@@ -696,7 +690,7 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
     case kTiled64x4: return launch_tiles<2, 2, 2, 2, 4, EXACT, GROUPED>(a, tiles(64), async, who, s);
     case kTiled64x2: return launch_tiles<2, 2, 2, 2, 2, EXACT, GROUPED>(a, tiles(64), async, who, s);
     case kTiled128x2: return launch_tiles<4, 4, 2, 2, 2, EXACT, GROUPED>(a, tiles(128), async, who, s);
-    case kTiled256: if constexpr (!EXACT) return launch_tiles_as<8, 4, 2, 4, 1, 2, EXACT, GROUPED, true>(a, tiles(256), who, s);
+    case kTiled256: if constexpr (!EXACT) return launch_tiles_as<8, 4, 2, 4, 1, EXACT, GROUPED, true>(a, tiles(256), who, s);
     default: return launch_tiles<4, 4, 2, 2, 1, EXACT, GROUPED>(a, tiles(128), async, who, s);
   }
 }
