@@ -668,11 +668,14 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   price[kDirect16x16] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 16, a);
   price[kDirect16x32] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 32, a);
   price[kDirect32x32] = direct_price(likely_tiles(32), std::min(32.0, likely_rows), 32, a);
-  price[kTiled64x4] = EXACT ? tiled(64, 1, 1.05, 1.4, 1, 4) : tiled(64, 1, 0.62, 1.0, 1, 4);
-  price[kTiled64x2] = EXACT ? tiled(64, 2, 0.62, 1.3, 1, 2) : tiled(64, 2, 0.36, 0.85, 1, 2);
+  constexpr double kSearch = GROUPED ? 2 : 0;                    // for the group, before a small tile's few steps
+  price[kTiled64x4] = EXACT ? tiled(64, 1, 1.05, 1.4, 1 + kSearch, 4) : tiled(64, 1, 0.62, 1.0, 1 + kSearch, 4);
+  price[kTiled64x2] = EXACT ? tiled(64, 2, 0.62, 1.3, 1 + kSearch, 2) : tiled(64, 2, 0.36, 0.85, 1 + kSearch, 2);
   price[kTiled128x2] = EXACT ? tiled(128, 1, 1.75, 1.75, 5, 2) : tiled(128, 1, 1.0, 1.0, 5, 2);
   price[kTiled128] = EXACT ? tiled(128, 2, 1.3, 1.9, 2, 1) : tiled(128, 2, 0.65, 1.08, 2, 1);
   price[kTiled256] = EXACT ? HUGE_VAL : tiled(256, 1, 1.6, 1.6, 6, 1);
+  if (GROUPED)                                                   // (weights that few rows share come from memory)
+    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.7;
   if (!aligned)                                                  // (five dwords for every four)
     for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.6;
   if (!async) {                                                  // through registers, where a step waits longer; the largest tile's sums leave none
