@@ -229,6 +229,63 @@ def test_grouped_product_agrees_with_the_product_of_each_group():
         first += size
 
 
+# ---------------------------------------------------------------- each kernel of the products
+D16, D32, D2 = "direct rows=16 columns=16", "direct rows=16 columns=32", "direct rows=32 columns=32"
+T4, T2, U2, U1, V = "tiled rows=64 columns=64 teams=4", "tiled rows=64 columns=64 teams=2", "tiled rows=128 columns=128 teams=2", "tiled rows=128 columns=128 teams=1", "tiled rows=256"
+KERNELS = [
+    # kernel, 32-bit output, rows, k, n, groups (0: one weight); rows of an odd k lie at odd addresses
+    (D16, False, 2, 104, 17, 0), (D32, False, 337, 108, 293, 0), (D2, False, 661, 104, 258, 0), (T4, False, 701, 896, 551, 0), (T2, False, 1133, 256, 772, 0),
+    (U2, False, 614, 6472, 3900, 0), (U1, False, 715, 384, 2712, 0), (V, False, 5431, 132, 2197, 0),
+    (D16, False, 2, 101, 17, 0), (D32, False, 244, 105, 402, 0), (D2, False, 484, 121, 353, 0), (T4, False, 619, 2995, 809, 0), (T2, False, 1003, 995, 970, 0),
+    (U2, False, 680, 4109, 4920, 0), (U1, False, 1704, 478, 1176, 0),
+    (D16, False, 3, 104, 17, 2), (D32, False, 361, 104, 277, 2), (D2, False, 737, 108, 227, 2), (T4, False, 1034, 2432, 296, 3), (T2, False, 1232, 1044, 819, 2),
+    (U2, False, 809, 4288, 2770, 5), (U1, False, 1174, 384, 874, 2), (V, False, 5889, 392, 2536, 3),
+    (D16, False, 2, 107, 18, 2), (D32, False, 431, 117, 239, 2), (D2, False, 1481, 105, 99, 3), (T2, False, 187, 1659, 1998, 8), (U2, False, 2234, 4181, 755, 8),
+    (U1, False, 1623, 745, 515, 2),
+    (D16, True, 2, 104, 17, 0), (D32, True, 325, 108, 311, 0), (D2, True, 747, 112, 225, 0), (T4, True, 823, 512, 781, 0), (T2, True, 1465, 640, 476, 0),
+    (U2, True, 1964, 1620, 1555, 0), (U1, True, 1425, 760, 1571, 0),
+    (D16, True, 2, 101, 17, 0), (D32, True, 334, 101, 311, 0), (D2, True, 388, 109, 452, 0), (T4, True, 914, 1565, 872, 0), (T2, True, 510, 1257, 1988, 0),
+    (U2, True, 1133, 1591, 1838, 0), (U1, True, 1982, 498, 1221, 0),
+    (D16, True, 2, 108, 19, 2), (D32, True, 435, 104, 227, 2), (D2, True, 956, 112, 168, 3), (T4, True, 1566, 1920, 206, 2), (T2, True, 2366, 512, 542, 3),
+    (U2, True, 3120, 1572, 930, 2), (U1, True, 3800, 128, 615, 2),
+    (D16, True, 3, 103, 17, 2), (D32, True, 924, 101, 98, 4), (D2, True, 964, 109, 167, 3), (T4, True, 822, 2521, 550, 2), (T2, True, 218, 837, 4147, 8),
+    (U2, True, 1202, 1579, 1818, 2), (U1, True, 1667, 377, 975, 2),
+]
+
+
+@gpu
+@pytest.mark.parametrize("case", KERNELS, ids=lambda c: "-".join(str(v) for v in c))
+def test_each_kernel_of_the_products(case):
+    """The launch rule's every kernel, at a size that the rule sends to it; a part of the rows and columns against 64 bits, all of them
+    against the bits of a second call."""
+    kernel, wide, rows, k, n, groups = case
+    print(f"case kernel {case}", flush=True)
+    gen = torch.Generator().manual_seed(rows + k + n)
+    x, xs, w, ws = random_operands(rows + 3 * k, rows, k, n, groups or None)
+    dtype = torch.float32 if wide else torch.bfloat16
+    on = [t.to(DEV) for t in (x, xs, w, ws)]
+    if groups:
+        cuts = torch.sort(torch.randint(0, rows + 1, (groups - 1,), generator=gen)).values.tolist()
+        sizes = [b - a for a, b in zip([0] + cuts, cuts + [rows])]
+        where = torch.tensor(sizes, device=DEV)
+        call = lambda: lk.lutkan_grouped_matmul_fp8(*on, where, dtype=dtype)  # noqa: E731
+    else:
+        sizes, (w, ws) = [rows], (t[None] for t in (w, ws))
+        call = lambda: lk.lutkan_matmul_fp8(*on, dtype=dtype)  # noqa: E731
+    y = call()
+    assert kernel in lk.lutkan_last_plan(), lk.lutkan_last_plan()
+    assert torch.equal(y, call())
+    columns = torch.unique(torch.cat([torch.randint(0, n, (150,), generator=gen), torch.tensor([0, n - 1])]))
+    first = 0
+    for e, size in enumerate(sizes):
+        if size:
+            at = first + torch.unique(torch.cat([torch.randint(0, size, (60,), generator=gen), torch.tensor([0, size - 1])]))
+            xv = decode(x.view(torch.uint8)[at].view(F8)) * spread(xs[at], (len(at), k), False)
+            wv = decode(w[e].view(torch.uint8)[columns].view(F8)) * spread(ws[e][columns // 128], (len(columns), k), False)
+            assert_product(y.cpu()[at][:, columns], xv @ wv.T, np.abs(xv) @ np.abs(wv).T, k)
+        first += size
+
+
 # ---------------------------------------------------------------- norm and conversion
 def step_of(v):
     """Distance of neighbouring e4m3 values around |v|."""
