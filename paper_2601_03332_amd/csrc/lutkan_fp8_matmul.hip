@@ -243,6 +243,8 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs &a, int64_t row)
 
 // A work-group computes 16 MT rows x 16 NT columns from global memory straight into registers; its waves take the blocks of k in turn,
 // and their sums meet in LDS in the waves' order.
+// Bound by what it reads, as no work-group shares with another: 16 rows of 4096 -> 4096 7.4 us a call (16 x 16: 256 work-groups, one to a
+// compute unit, weights 17 MB and as much of x again; 6.2 if all rows of x were one, 9.0 with 16 x 32); one row 5.1.
 template <int MT, int NT, bool EXACT, bool GROUPED, bool ALIGNED>
 __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_kernel(const ProductArgs a) {
   extern __shared__ __align__(16) f32x4 s_part[];                // [wave][row tile][column tile][lane]
@@ -378,6 +380,10 @@ int launch_direct(ProductArgs a, int64_t row_tiles, bool aligned, const char *wh
 // lie in different banks (no conflict counted).
 //   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and
 //   offsets that fit 32 bits.  Otherwise, and for a last block that is not whole, through registers.
+// What it measured, into bf16, 8192 rows of 4096 -> 4096: 256 x 256 outputs 119 - 124 us on the same inputs again and again, 127 - 137 on three sets
+// in turn (2.3 - 2.0 PFLOP/s; a library product of such codes with one scale for all 94), 128 x 128 157.  Matrix cores 0.45 busy: copies alone
+// take 90 us, products and sums alone 105; codes of zeros 94 where random ones take 118, so that power decides too.  Into fp32
+// (128 x 128) 259.  Teams: 256 rows of the same 11.3 us with four on 64 x 64, 22 without; 128 x 128 18.6 with two, 26.5 without.
 __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ ((row >> 1) & 7); }
 
 // As copy16_global_to_lds_at, four bytes a lane.
@@ -634,6 +640,8 @@ bool copies_fit(const ProductArgs &a) {                          // the rows' of
 //   tiled    rounds of as many tiles as fit the compute units, a tile's steps over k: `one` where there is one to a compute unit, `all` where
 //            there are `slots`, and `ends` before and behind the steps.  Where the number of tiles is a guess (groups) and two fit a compute
 //            unit, a round that is begun counts by its part.
+// What the choice is worth, us: 16 rows of 4096 -> 4096 7.2 with 16 x 16, 9.0 with 16 x 32; 256 of them 11.3 with four teams on 64 x 64, 11.6 with two, 26.5
+// with 128 x 128; 614 of 6472 -> 3900 49 with two teams on 128 x 128, 60 with one, 65 with two on 64 x 64 (into fp32 5076 of 7936 -> 711 64, 95, 83).
 inline double direct_price(double row_tiles, double rows_of_tile, int columns, const ProductArgs &a) {
   const double work_groups = row_tiles * ((a.n + columns - 1) / columns);
   return work_groups * (rows_of_tile + columns) * a.k / (9e6 * std::min(1.0, work_groups / 256));
