@@ -635,7 +635,9 @@ bool copies_fit(const ProductArgs &a) {                          // the rows' of
 }
 
 // What a launch takes beyond an empty one, in us, for the kernels' choice; fitted to times from 1 to 8192 rows, 128 to 8192 inputs and
-// 256 to 8192 outputs (within a fifth of them where two kernels come near each other).
+// 256 to 8192 outputs (within a fifth of them where two kernels come near each other; a third with rows at odd addresses).  Such rows
+// into 16 bits have a price of their own for each step: 120 drawn calls 0.95 of the time with the factors that 32 bits keep (38 changed their kernel, 0.56 -
+// 1.36 each); for 32 bits the same did not pay (1.10 over the calls that changed).
 //   direct   what its work-groups read, each its own: 9 MB/us over the whole GPU
 //   tiled    rounds of as many tiles as fit the compute units, a tile's steps over k: `one` where there is one to a compute unit, `all` where
 //            there are `slots`, and `ends` before and behind the steps.  Where the number of tiles is a guess (groups) and two fit a compute
@@ -669,7 +671,8 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows);
   const double end_block = a.k % kScaleBlock ? 2.5 : 0;          // (read, put and multiplied behind the others)
   const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
-    return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one, all, ends + end_block, std::ceil(a.k / kScaleBlock / (double)teams), GROUPED);
+    const double step = async || EXACT ? 1 : side == 64 ? 1.75 : 1.5;     // through registers a step waits longer
+    return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one * step, all * step, ends + end_block, std::ceil(a.k / kScaleBlock / (double)teams), GROUPED);
   };
   enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kKernels };
   double price[kKernels];
@@ -685,11 +688,11 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   if (GROUPED)                                                   // (weights that few rows share come from memory)
     for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.7;
   if (!aligned)                                                  // (five dwords for every four)
-    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.6;
-  if (!async) {                                                  // through registers, where a step waits longer; the largest tile's sums leave none
+    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= EXACT ? 1.6 : 2;
+  if (!async) price[kTiled256] = HUGE_VAL;                       // (its sums leave no registers to copy through)
+  if (!async && EXACT) {                                         // (through registers: steps and ends in one)
     price[kTiled64x4] *= 2, price[kTiled64x2] *= 2;
     price[kTiled128x2] *= 1.5, price[kTiled128] *= 1.5;
-    price[kTiled256] = HUGE_VAL;
   }
   if (tiles(16) > 65535) price[kDirect16x16] = price[kDirect16x32] = HUGE_VAL;
   if (tiles(32) > 65535) price[kDirect32x32] = HUGE_VAL;

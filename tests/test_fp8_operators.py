@@ -240,8 +240,8 @@ KERNELS = [
     (U2, False, 680, 4109, 4920, 0), (U1, False, 1704, 478, 1176, 0),
     (D16, False, 3, 104, 17, 2), (D32, False, 361, 104, 277, 2), (D2, False, 737, 108, 227, 2), (T4, False, 1034, 2432, 296, 3), (T2, False, 1232, 1044, 819, 2),
     (U2, False, 809, 4288, 2770, 5), (U1, False, 1174, 384, 874, 2), (V, False, 5889, 392, 2536, 3),
-    (D16, False, 2, 107, 18, 2), (D32, False, 431, 117, 239, 2), (D2, False, 1481, 105, 99, 3), (T2, False, 187, 1659, 1998, 8), (U2, False, 2234, 4181, 755, 8),
-    (U1, False, 1623, 745, 515, 2),
+    (D16, False, 2, 107, 18, 2), (D32, False, 431, 117, 239, 2), (D2, False, 1481, 105, 99, 3), (T2, False, 187, 1659, 1998, 8), (T2, False, 2234, 4181, 755, 8),
+    (T2, False, 1623, 745, 515, 2), (U2, False, 1626, 2406, 1448, 2), (U1, False, 1454, 241, 641, 2),
     (D16, True, 2, 104, 17, 0), (D32, True, 325, 108, 311, 0), (D2, True, 747, 112, 225, 0), (T4, True, 823, 512, 781, 0), (T2, True, 1465, 640, 476, 0),
     (U2, True, 1964, 1620, 1555, 0), (U1, True, 1425, 760, 1571, 0),
     (D16, True, 2, 101, 17, 0), (D32, True, 334, 101, 311, 0), (D2, True, 388, 109, 452, 0), (T4, True, 914, 1565, 872, 0), (T2, True, 510, 1257, 1988, 0),
