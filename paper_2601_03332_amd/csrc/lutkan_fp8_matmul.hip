@@ -385,7 +385,7 @@ int launch_direct(ProductArgs a, int64_t row_tiles, bool aligned, const char *wh
 //   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and
 //   offsets that fit 32 bits.  Otherwise, and for a last block that is not whole, through registers.
 // What it measured, into bf16, 8192 rows of 4096 -> 4096: 256 x 256 outputs 119 - 124 us on the same inputs again and again, 127 - 137 on three sets
-// in turn (2.3 - 2.0 PFLOP/s; a library product of such codes with one scale for all 94), 128 x 128 157.  Matrix cores 0.45 busy: copies alone
+// in turn (2.3 - 2.0 PFLOP/s; a library product of such codes with one scale for all 94), 128 x 128 157.  Matrix cores 0.46 busy: copies alone
 // take 90 us, products and sums alone 105; codes of zeros 94 where random ones take 118, so that power decides too.  Into fp32
 // (128 x 128) 259.  Teams: 256 rows of the same 11.3 us with four on 64 x 64, 22 without; 128 x 128 18.6 with two, 26.5 without.
 __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ ((row >> 1) & 7); }
