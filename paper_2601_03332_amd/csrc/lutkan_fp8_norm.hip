@@ -246,23 +246,31 @@ extern "C" int lutkan_rmsnorm_fp8(const lutkan_rmsnorm_fp8_args *p, void *hip_st
   if (p->rows >= 2048 && waves <= 4) { chunks = waves; waves = 1; }
   else if (p->rows >= 1024 && waves <= 16) { chunks = waves > 8 ? 4 : waves > 4 ? 2 : 1; waves = (waves + chunks - 1) / chunks; }
   while (waves > 16) { chunks *= 2; waves = (p->width + 512 * chunks - 1) / (512 * chunks); }
-  const int64_t groups = waves == 1 ? (p->rows + kRowsOfGroup - 1) / kRowsOfGroup : p->rows;
-  if (groups > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many rows", who);
-  NormArgs a;
-  a.x = static_cast<const unsigned char *>(p->x); a.residual = static_cast<const unsigned char *>(p->residual);
-  a.weight = static_cast<const unsigned char *>(p->weight); a.residual_out = static_cast<unsigned char *>(p->residual_out);
-  a.codes = static_cast<unsigned char *>(p->codes); a.scales = p->scales;
-  a.x_stride = (int32_t)p->x_stride; a.residual_stride = (int32_t)p->residual_stride; a.residual_out_stride = (int32_t)p->residual_out_stride;
-  a.codes_stride = (int32_t)p->codes_stride; a.scales_stride = (int32_t)p->scales_stride; a.row_waves = waves;
-  a.rows = p->rows; a.width = p->width; a.weight_type = p->weight_type; a.eps = p->eps; a.inverse_width = 1.0f / (float)p->width;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const unsigned threads = waves == 1 ? 64u * kRowsOfGroup : (unsigned)waves * 64u;
-  switch (p->x_type) {
-    case LUTKAN_F32: launch_norm_of<LUTKAN_F32>(a, p->residual_type, chunks, (unsigned)groups, threads, s); break;
-    case LUTKAN_F16: launch_norm_of<LUTKAN_F16>(a, p->residual_type, chunks, (unsigned)groups, threads, s); break;
-    default: launch_norm_of<LUTKAN_BF16>(a, p->residual_type, chunks, (unsigned)groups, threads, s); break;
+  const int group_rows = waves == 1 ? kRowsOfGroup : 1;
+  const int64_t launch_rows = kMaxLaunchThreads / threads * group_rows;          // (more rows: more launches)
+  const int64_t residual_bytes = p->residual ? type_bytes(p->residual_type) : 0;
+  for (int64_t first = 0; first < p->rows; first += launch_rows) {
+    NormArgs a;
+    a.x = static_cast<const unsigned char *>(p->x) + first * p->x_stride * type_bytes(p->x_type);
+    a.residual = static_cast<const unsigned char *>(p->residual) + first * p->residual_stride * residual_bytes;
+    a.weight = static_cast<const unsigned char *>(p->weight);
+    a.residual_out = static_cast<unsigned char *>(p->residual_out) + first * p->residual_out_stride * residual_bytes;
+    a.codes = static_cast<unsigned char *>(p->codes) + first * p->codes_stride; a.scales = p->scales + first * p->scales_stride;
+    a.x_stride = (int32_t)p->x_stride; a.residual_stride = (int32_t)p->residual_stride; a.residual_out_stride = (int32_t)p->residual_out_stride;
+    a.codes_stride = (int32_t)p->codes_stride; a.scales_stride = (int32_t)p->scales_stride; a.row_waves = waves;
+    a.rows = std::min(p->rows - first, launch_rows); a.width = p->width; a.weight_type = p->weight_type;
+    a.eps = p->eps; a.inverse_width = 1.0f / (float)p->width;
+    const unsigned groups = (unsigned)((a.rows + group_rows - 1) / group_rows);
+    switch (p->x_type) {
+      case LUTKAN_F32: launch_norm_of<LUTKAN_F32>(a, p->residual_type, chunks, groups, threads, s); break;
+      case LUTKAN_F16: launch_norm_of<LUTKAN_F16>(a, p->residual_type, chunks, groups, threads, s); break;
+      default: launch_norm_of<LUTKAN_BF16>(a, p->residual_type, chunks, groups, threads, s); break;
+    }
+    if (int rc = check_launch(who)) return rc;
   }
-  return check_launch(who);
+  return LUTKAN_OK;
 }
 
 extern "C" int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t matrices, int32_t n, int32_t k, int64_t stride, int64_t matrix_stride,

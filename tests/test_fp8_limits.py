@@ -1,0 +1,24 @@
+"""The 8-bit operators at the ends of their ranges."""
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2601_03332_amd as lk  # noqa: E402
+from test_fp8_operators import DEV, gpu  # noqa: E402
+
+
+# ---------------------------------------------------------------- more than one launch holds (fewer than 2^32 threads)
+@gpu
+def test_norm_of_more_rows_than_one_launch_holds():
+    """A wave a row: 2^26 rows are 2^32 threads.  The rows on both sides of every 2^24 rows as a short call gives them: a launch
+    of 2^32 threads and more runs a part of them, without an error."""
+    rows, width = (1 << 26) + 4099, 8
+    print(f"case norm {rows} x {width}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(rows, width, generator=gen, device=DEV, dtype=torch.bfloat16)
+    residual = torch.randn(rows, width, generator=gen, device=DEV, dtype=torch.float16)
+    weight = 1 + 0.1 * torch.randn(width, generator=gen, device=DEV)
+    codes, scales, out = lk.lutkan_rmsnorm_fp8(x, weight, residual=residual)
+    for end in [i << 24 for i in range(1, 5)] + [2100, rows]:
+        at = slice(end - 2100, min(end + 2100, rows))
+        part = lk.lutkan_rmsnorm_fp8(x[at], weight, residual=residual[at])
+        assert torch.equal(codes[at].view(torch.uint8), part[0].view(torch.uint8)) and torch.equal(scales[at], part[1]) and torch.equal(out[at], part[2])
