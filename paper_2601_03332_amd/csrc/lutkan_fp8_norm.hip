@@ -161,6 +161,7 @@ struct QuantiseArgs {
   float *scales;
   int64_t w_stride, w_matrix_stride;
   int32_t n, k;
+  unsigned first;                                                // block of the launch's first work-group
 };
 
 // A work-group of 256 threads converts one block: 16 lanes a row of 128 columns, eight rows each thread, all in registers between
@@ -170,7 +171,7 @@ template <int X>
 __global__ __launch_bounds__(256) void lutkan_quantise_fp8_kernel(const QuantiseArgs a) {
   __shared__ unsigned s_largest[4];
   const unsigned column_blocks = (a.k + kScaleBlock - 1) / kScaleBlock, row_blocks = (a.n + kScaleBlock - 1) / kScaleBlock;
-  const unsigned column_block = blockIdx.x % column_blocks, rest = blockIdx.x / column_blocks, row_block = rest % row_blocks;
+  const unsigned block = a.first + blockIdx.x, column_block = block % column_blocks, rest = block / column_blocks, row_block = rest % row_blocks;
   const int64_t matrix = rest / row_blocks;
   const int col = column_block * kScaleBlock + 8 * (threadIdx.x & 15), row0 = row_block * kScaleBlock + (threadIdx.x >> 4);
   const unsigned char *w = a.w + (matrix * a.w_matrix_stride + col) * type_bytes(X);
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(256) void lutkan_quantise_fp8_kernel(const Quantise
   __syncthreads();
   largest = max(max(s_largest[0], s_largest[1]), max(s_largest[2], s_largest[3]));
   const float scale = block_scale(largest);
-  if (threadIdx.x == 0) a.scales[blockIdx.x] = scale;            // the blocks' order is the scales'
+  if (threadIdx.x == 0) a.scales[block] = scale;                // the blocks' order is the scales'
   unsigned char *codes = a.codes + matrix * a.n * a.k + col;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -286,12 +287,17 @@ extern "C" int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t mat
   a.w_stride = stride; a.w_matrix_stride = matrix_stride; a.n = n; a.k = k;
   const int64_t per_matrix = scale_blocks(n) * scale_blocks(k);
   if (matrices > 0x7fffffff / per_matrix) return fail(LUTKAN_EUNSUPPORTED, "%s: too many blocks", who);
-  const dim3 groups((unsigned)(matrices * per_matrix));
+  const int64_t all = matrices * per_matrix, launch_blocks = kMaxLaunchThreads / 256;      // (more blocks: more launches)
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  switch (type) {
-    case LUTKAN_F32: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_F32>, groups, dim3(256), 0, s, a); break;
-    case LUTKAN_F16: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_F16>, groups, dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_BF16>, groups, dim3(256), 0, s, a); break;
+  for (int64_t first = 0; first < all; first += launch_blocks) {
+    a.first = (unsigned)first;
+    const dim3 groups((unsigned)std::min(all - first, launch_blocks));
+    switch (type) {
+      case LUTKAN_F32: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_F32>, groups, dim3(256), 0, s, a); break;
+      case LUTKAN_F16: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_F16>, groups, dim3(256), 0, s, a); break;
+      default: hipLaunchKernelGGL(lutkan_quantise_fp8_kernel<LUTKAN_BF16>, groups, dim3(256), 0, s, a); break;
+    }
+    if (int rc = check_launch(who)) return rc;
   }
-  return check_launch(who);
+  return LUTKAN_OK;
 }

@@ -22,3 +22,15 @@ def test_norm_of_more_rows_than_one_launch_holds():
         at = slice(end - 2100, min(end + 2100, rows))
         part = lk.lutkan_rmsnorm_fp8(x[at], weight, residual=residual[at])
         assert torch.equal(codes[at].view(torch.uint8), part[0].view(torch.uint8)) and torch.equal(scales[at], part[1]) and torch.equal(out[at], part[2])
+
+
+@gpu
+def test_weights_of_more_blocks_than_one_launch_holds():
+    """A work-group of 256 threads a block: 2^24 blocks are 2^32 threads."""
+    matrices = (1 << 24) + 3
+    print(f"case weights {matrices} of 1 x 1", flush=True)
+    w = torch.randn(matrices, 1, 1, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV, dtype=torch.bfloat16)
+    codes, scales = lk.lutkan_quantise_fp8(w)
+    expected = (w.float().abs() / torch.full((1,), 448.0, device=DEV)).clamp(min=2.0 ** -126)
+    assert bool(((scales - expected).abs() <= 2.0 ** -22 * expected).all())
+    assert torch.equal(codes.view(torch.uint8), torch.where(w < 0, 0xfe, 0x7e).to(torch.uint8).masked_fill_(w == 0, 0))
