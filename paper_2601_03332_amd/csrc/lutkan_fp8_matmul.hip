@@ -669,7 +669,6 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
     const double some = (double)std::min<int64_t>(groups, a.rows), each = (double)a.rows / some;
     return some * std::max(1.0, each / height + (each > 1 ? 0.6 : 0.0));
   };
-  if (tiles(64) * ((a.n + 63) / 64) > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   lutkan::plan_clear();
   const bool aligned = rows_aligned(a), async = aligned && copies_fit<GROUPED>(a);
   const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows);
@@ -700,7 +699,14 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   }
   if (tiles(16) > 65535) price[kDirect16x16] = price[kDirect16x32] = HUGE_VAL;
   if (tiles(32) > 65535) price[kDirect32x32] = HUGE_VAL;
+  const auto beyond_a_launch = [&](int side, int threads) { return tiles(side) * ((a.n + side - 1) / side) > kMaxLaunchThreads / threads; };
+  if (beyond_a_launch(64, 1024)) price[kTiled64x4] = HUGE_VAL;
+  if (beyond_a_launch(64, 512)) price[kTiled64x2] = HUGE_VAL;
+  if (beyond_a_launch(128, 512)) price[kTiled128x2] = HUGE_VAL;
+  if (beyond_a_launch(128, 256)) price[kTiled128] = HUGE_VAL;
+  if (beyond_a_launch(256, 512)) price[kTiled256] = HUGE_VAL;
   const int pick = (int)(std::min_element(price, price + kKernels) - price);
+  if (price[pick] == HUGE_VAL) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   switch (pick) {
     case kDirect16x16: return launch_direct<1, 1, EXACT, GROUPED>(a, tiles(16), aligned, who, s);
     case kDirect16x32: return launch_direct<1, 2, EXACT, GROUPED>(a, tiles(16), aligned, who, s);

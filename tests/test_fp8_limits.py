@@ -1,9 +1,12 @@
 """The 8-bit operators at the ends of their ranges."""
+import ctypes as C
+
 import pytest
 
 torch = pytest.importorskip("torch")
 import paper_2601_03332_amd as lk  # noqa: E402
-from test_fp8_operators import DEV, gpu  # noqa: E402
+from paper_2601_03332_amd import binding  # noqa: E402
+from test_fp8_operators import DEV, F8, gpu  # noqa: E402
 
 
 # ---------------------------------------------------------------- more than one launch holds (fewer than 2^32 threads)
@@ -34,3 +37,32 @@ def test_weights_of_more_blocks_than_one_launch_holds():
     expected = (w.float().abs() / torch.full((1,), 448.0, device=DEV)).clamp(min=2.0 ** -126)
     assert bool(((scales - expected).abs() <= 2.0 ** -22 * expected).all())
     assert torch.equal(codes.view(torch.uint8), torch.where(w < 0, 0xfe, 0x7e).to(torch.uint8).masked_fill_(w == 0, 0))
+
+
+@gpu
+def test_product_of_more_rows_than_one_launch_of_small_tiles_holds():
+    """2^23 work-groups of 512 threads are 2^32: such calls take larger tiles.  The rows are overlapping windows, four codes apart, of one line
+    of codes 1, -1 and 0, whose sums are whole numbers and have no rounding."""
+    rows, k = (1 << 29) + 77, 256
+    print(f"case product {rows} x {k} -> 1", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    codes = torch.tensor([0x00, 0x38, 0xb8], dtype=torch.uint8, device=DEV)
+    line = codes[torch.randint(0, 3, (1 << 16,), generator=gen, device=DEV)].repeat((4 * rows + k) // (1 << 16) + 1)
+    w = codes[torch.randint(0, 3, (1, k), generator=gen, device=DEV)].view(F8)
+    one = torch.ones(1, 2, device=DEV)
+    x = line.as_strided((rows, k), (4, 1)).view(F8)
+    y = lk.lutkan_matmul_fp8(x, one.expand(rows, 2), w, one)
+    short = lk.lutkan_matmul_fp8(x[:(1 << 14) + 100], one.expand((1 << 14) + 100, 2), w, one)
+    assert int(short.abs().max()) > 0
+    assert torch.equal(short[:100], short[1 << 14:])               # (the line repeats itself)
+    assert torch.equal(y, short[:1 << 14].repeat(rows // (1 << 14) + 1, 1)[:rows])
+
+
+def test_products_that_no_launch_holds_are_refused():
+    lib = lk.load_library()
+    rows = (1 << 31) - 1
+    a = binding._MatmulFp8Args(4096, 4096, 4096, 4096, 4096, rows, 1, 1, 1, 1, 1, rows, 1, 1, 0, 1, 4096, None, 8, 8)
+    assert lib.lutkan_matmul_fp8(C.byref(a), None) == -5, lk.lutkan_last_error()
+    rows, groups, n = 1 << 24, 1 << 17, 1 << 14
+    a = binding._MatmulFp8Args(4096, 4096, 4096, 4096, 4096, rows, 16, 1, 16, 16 * n, n, rows, 16, n, 2, groups, 4096, None, 8, 8)
+    assert lib.lutkan_grouped_matmul_fp8(C.byref(a), None) == -5, lk.lutkan_last_error()
