@@ -787,6 +787,12 @@ def _check_matrix(who, what, t, shape, device, dtype=None):
         raise LutKanError(f"{who}: {what} must have contiguous columns")
 
 
+def _check_length(who, what, n):
+    """Lengths that the library takes as 32-bit numbers (ctypes would keep their low bits)."""
+    if n > 2147483647:
+        raise LutKanError(f"{who}: {what} of {n}, at most 2147483647")
+
+
 def _row_stride(t):
     """Elements from one row of a matrix to the next; that of a dimension of one row is arbitrary and not used."""
     return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
@@ -810,6 +816,7 @@ def lutkan_rmsnorm_fp8(x, weight, residual=None, eps: float = 1e-6, residual_out
     who, torch = "lutkan_rmsnorm_fp8", _torch()
     _check_matrix(who, "x", x, (None, None), None)
     rows, width = x.shape
+    _check_length(who, "a width", width)
     _check_matrix(who, "weight", weight, (width,), x.device)
     if residual is not None:
         _check_matrix(who, "residual", residual, (rows, width), x.device)
@@ -842,6 +849,8 @@ def lutkan_quantise_fp8(weight):
     who, torch = "lutkan_quantise_fp8", _torch()
     _check_matrix(who, "weight", weight, (None,) * (3 if isinstance(weight, torch.Tensor) and weight.dim() == 3 else 2), None)
     n, k = weight.shape[-2:]
+    _check_length(who, "outputs", n)
+    _check_length(who, "inputs", k)
     codes = torch.empty(weight.shape, dtype=torch.float8_e4m3fn, device=weight.device)
     scales = torch.empty((*weight.shape[:-2], _blocks(n), _blocks(k)), dtype=torch.float32, device=weight.device)
     with torch.cuda.device(weight.device):
@@ -859,6 +868,8 @@ def _matmul_fp8(who, x, x_scales, weight, weight_scales, y, dtype, rows, experts
     _check_matrix(who, "x_scales", x_scales, (x.shape[0], _blocks(k)), device, torch.float32)
     _check_matrix(who, "weight", weight, (None, None, k) if experts else (None, k), device, torch.float8_e4m3fn)
     n = weight.shape[-2]
+    for what, length in (("inputs", k), ("outputs", n), ("weights", weight.shape[0] if experts else 1)):
+        _check_length(who, what, length)
     _check_matrix(who, "weight_scales", weight_scales, (*weight.shape[:-2], _blocks(n), _blocks(k)), device, torch.float32)
     if not weight_scales.is_contiguous():
         raise LutKanError(f"{who}: weight_scales must be contiguous")

@@ -66,3 +66,21 @@ def test_products_that_no_launch_holds_are_refused():
     rows, groups, n = 1 << 24, 1 << 17, 1 << 14
     a = binding._MatmulFp8Args(4096, 4096, 4096, 4096, 4096, rows, 16, 1, 16, 16 * n, n, rows, 16, n, 2, groups, 4096, None, 8, 8)
     assert lib.lutkan_grouped_matmul_fp8(C.byref(a), None) == -5, lk.lutkan_last_error()
+
+
+# ---------------------------------------------------------------- lengths beyond 32 bits
+@gpu
+def test_the_binding_refuses_lengths_beyond_32_bits():
+    """The library's widths, inputs, outputs and groups are 32-bit numbers: a longer tensor is refused, not cut to its low bits."""
+    def refused(f, *args, **kwargs):
+        with pytest.raises(lk.LutKanError, match="2147483647"):
+            f(*args, **kwargs)
+    much = (1 << 32) + 1                                           # cut to 32 bits: 1
+    w = torch.zeros(1, 1, dtype=torch.bfloat16, device=DEV)
+    refused(lk.lutkan_quantise_fp8, w.expand(much, 1))
+    refused(lk.lutkan_quantise_fp8, w[None].expand(2, much, 1))
+    one, scale = torch.zeros(1, 1, dtype=torch.uint8, device=DEV).view(F8), torch.ones(1, 1, device=DEV)
+    refused(lk.lutkan_matmul_fp8, one, scale, one.expand(much, 1), torch.ones(-(-much // 128), 1, device=DEV))
+    refused(lk.lutkan_grouped_matmul_fp8, one, scale, one[None].expand(1, much, 1), torch.ones(1, -(-much // 128), 1, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV))
+    wide = torch.empty((1 << 32) + 128, dtype=torch.bfloat16, device=DEV)
+    refused(lk.lutkan_rmsnorm_fp8, wide[None], wide)
