@@ -170,12 +170,12 @@ struct QuantiseArgs {
 template <int X>
 __global__ __launch_bounds__(256) void lutkan_quantise_fp8_kernel(const QuantiseArgs a) {
   __shared__ unsigned s_largest[4];
-  const unsigned column_blocks = (a.k + kScaleBlock - 1) / kScaleBlock, row_blocks = (a.n + kScaleBlock - 1) / kScaleBlock;
+  const unsigned column_blocks = ((unsigned)a.k + kScaleBlock - 1) / kScaleBlock, row_blocks = ((unsigned)a.n + kScaleBlock - 1) / kScaleBlock;
   const unsigned block = a.first + blockIdx.x, column_block = block % column_blocks, rest = block / column_blocks, row_block = rest % row_blocks;
   const int64_t matrix = rest / row_blocks;
   const int col = column_block * kScaleBlock + 8 * (threadIdx.x & 15), row0 = row_block * kScaleBlock + (threadIdx.x >> 4);
   const unsigned char *w = a.w + (matrix * a.w_matrix_stride + col) * type_bytes(X);
-  const bool whole = col + 8 <= a.k;
+  const bool whole = a.k - col >= 8;                             // (col + 8 can pass 2^31)
   float v[8][8];
   if (whole) {                                                   // all loads first; rows behind the last are the last again
     Raw8<X> raw[8];

@@ -84,3 +84,23 @@ def test_the_binding_refuses_lengths_beyond_32_bits():
     refused(lk.lutkan_grouped_matmul_fp8, one, scale, one[None].expand(1, much, 1), torch.ones(1, -(-much // 128), 1, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV))
     wide = torch.empty((1 << 32) + 128, dtype=torch.bfloat16, device=DEV)
     refused(lk.lutkan_rmsnorm_fp8, wide[None], wide)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(1, (1 << 31) - 1), ((1 << 31) - 1, 1)], ids=str)
+def test_weights_of_the_longest_rows_and_columns(shape):
+    """2^31 - 1 inputs or outputs: places near the end pass 2^31 when eight columns, or a block, are added.  Nothing behind the codes and
+    scales is written."""
+    n, k = shape
+    print(f"case weights {shape}", flush=True)
+    count, last = n * k, (n * k - 1) // 128 * 128
+    w = torch.ones(count, dtype=torch.bfloat16, device=DEV)
+    w[-1] = -2.0
+    codes = torch.full((count + 64,), 0x55, dtype=torch.uint8, device=DEV)
+    scales = torch.full((last // 128 + 2,), 7.0, device=DEV)
+    lib = lk.load_library()
+    assert lib.lutkan_quantise_fp8(w.data_ptr(), 2, 1, n, k, k, count, codes.data_ptr(), scales.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    assert bool((codes[:last] == 0x7e).all()) and bool((codes[last:count - 1] == 0x76).all()) and int(codes[count - 1]) == 0xfe      # 448; 224, -448
+    assert bool((codes[count:] == 0x55).all())
+    assert bool((scales[:-2] - 1 / 448).abs().max() <= 2.0 ** -31) and abs(float(scales[-2]) * 448 - 2) <= 2.0 ** -20 and float(scales[-1]) == 7.0
