@@ -401,6 +401,7 @@ typedef enum { LUTKAN_F32 = 0, LUTKAN_F16 = 1, LUTKAN_BF16 = 2 } lutkan_type;
 #define LUTKAN_FP8_MAX_WIDTH 32768          /* columns of a row that is normalised */
 #define LUTKAN_FP8_MAX_INPUTS 1048576       /* inputs or outputs of a product */
 #define LUTKAN_FP8_MAX_GROUPED_ROWS 16777216    /* rows of a grouped product */
+#define LUTKAN_FP8_MAX_GROUPS 1048576       /* its groups; every work-group looks through their sizes, 64 at a time */
 
 /* The residual's addition, the root-mean-square norm and the conversion to codes, in one pass over x [rows][width]:
  *     h = x + residual (fp32),   y = h / sqrt(mean(h^2) + eps) * weight,   codes and scales of y

@@ -757,6 +757,7 @@ extern "C" int lutkan_grouped_matmul_fp8(const lutkan_matmul_fp8_args *p, void *
   ProductArgs a;
   if (int rc = check_product(p, who, &a)) return rc;
   if (p->groups < 1) return fail(LUTKAN_EINVAL, "%s: %d groups", who, p->groups);
+  if (p->groups > LUTKAN_FP8_MAX_GROUPS) return fail(LUTKAN_EUNSUPPORTED, "%s: %d groups, at most %d", who, p->groups, LUTKAN_FP8_MAX_GROUPS);
   if (p->rows == 0) return LUTKAN_OK;
   if (!p->group_sizes) return fail(LUTKAN_EINVAL, "%s: null group_sizes", who);
   if ((p->group_sizes_bytes != 4 && p->group_sizes_bytes != 8) || (p->row_index && p->row_index_bytes != 4 && p->row_index_bytes != 8))

@@ -104,3 +104,31 @@ def test_weights_of_the_longest_rows_and_columns(shape):
     assert bool((codes[:last] == 0x7e).all()) and bool((codes[last:count - 1] == 0x76).all()) and int(codes[count - 1]) == 0xfe      # 448; 224, -448
     assert bool((codes[count:] == 0x55).all())
     assert bool((scales[:-2] - 1 / 448).abs().max() <= 2.0 ** -31) and abs(float(scales[-2]) * 448 - 2) <= 2.0 ** -20 and float(scales[-1]) == 7.0
+
+
+def test_more_groups_than_the_search_counts_are_refused():
+    """The search for a tile's group steps through the sizes in 32 bits: near 2^31 groups the step passes them and does not end.  Long before
+    that a work-group's walk takes longer than its products."""
+    for groups in ((1 << 20) + 1, (1 << 31) - 1):
+        a = binding._MatmulFp8Args(4096, 4096, 4096, 4096, 4096, 1, 16, 1, 16, 0, 1, 1, 16, 1, 2, groups, 4096, None, 4, 8)
+        assert lk.load_library().lutkan_grouped_matmul_fp8(C.byref(a), None) == -5, lk.lutkan_last_error()
+        assert "groups" in lk.lutkan_last_error()
+
+
+@gpu
+def test_the_most_groups():
+    """2^20 groups of one row, none or two, all with the same weight: the product with one weight, bit for bit (whole numbers)."""
+    groups, k, n = 1 << 20, 16, 4
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    sizes = torch.zeros(groups, dtype=torch.int32, device=DEV)
+    sizes[torch.randint(0, groups, (40,), generator=gen, device=DEV)] = 1
+    sizes[groups - 1] = 2
+    rows = int(sizes.sum()) + 1                                    # and one behind the last group
+    print(f"case groups {groups}, rows {rows}", flush=True)
+    codes = torch.tensor([0x00, 0x38, 0xb8], dtype=torch.uint8, device=DEV)
+    x, w = (codes[torch.randint(0, 3, shape, generator=gen, device=DEV)] for shape in ((rows, k), (n, k)))
+    one = torch.ones(1, 1, device=DEV)
+    y = lk.lutkan_grouped_matmul_fp8(x.view(F8), one.expand(rows, 1), w.view(F8).expand(groups, n, k), torch.ones(groups, 1, 1, device=DEV), sizes)
+    expected = lk.lutkan_matmul_fp8(x.view(F8), one.expand(rows, 1), w.view(F8), one)
+    expected[rows - 1] = 0
+    assert torch.equal(y, expected)
