@@ -25,8 +25,10 @@ class ExpertBlock:
 
     def __init__(self, norm, router, experts, layer, top: int = 2, eps: float = 1e-6):
         from . import LutKanError, lutkan_quantise_fp8
-        if experts.shape[1] != layer.d or experts.shape[2] != layer.m or not 1 <= top <= experts.shape[0]:
+        if experts.dim() != 3 or experts.shape[1] != layer.d or experts.shape[2] != layer.m or not 1 <= top <= experts.shape[0]:
             raise LutKanError("ExpertBlock: experts are [experts, layer.d, layer.m], top is at most their number")
+        if tuple(router.shape) != (experts.shape[0], layer.m):           # (an expert that is not there would be counted out of bounds)
+            raise LutKanError(f"ExpertBlock: router is [experts, layer.m], here [{experts.shape[0]}, {layer.m}]")
         self.norm, self.layer, self.top, self.eps = norm, layer, top, eps
         self.router, self.experts = lutkan_quantise_fp8(router), lutkan_quantise_fp8(experts)
 

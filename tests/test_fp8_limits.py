@@ -132,3 +132,16 @@ def test_the_most_groups():
     expected = lk.lutkan_matmul_fp8(x.view(F8), one.expand(rows, 1), w.view(F8), one)
     expected[rows - 1] = 0
     assert torch.equal(y, expected)
+
+
+# ---------------------------------------------------------------- the block
+def test_the_block_refuses_a_router_that_does_not_fit_its_experts():
+    """A router of more rows than there are experts would pick experts that do not exist."""
+    from types import SimpleNamespace
+    from paper_2601_03332_amd.expert_block import ExpertBlock
+    layer, norm = SimpleNamespace(d=6, m=10), torch.ones(10)
+    for shape in ((5, 10), (3, 10), (4, 9), (40,)):
+        with pytest.raises(lk.LutKanError, match="router is"):
+            ExpertBlock(norm, torch.zeros(shape), torch.zeros(4, 6, 10), layer)
+    with pytest.raises(lk.LutKanError, match="experts are"):
+        ExpertBlock(norm, torch.zeros(4, 10), torch.zeros(6, 10), layer)
