@@ -330,7 +330,7 @@ int launch_spline_tiled_np(const SplineEdgeArgs &ea, hipStream_t s) {
   constexpr int RW = (64 / LPR) * NP;
   const int bytes = ea.rows * 4 * LPR * 4;
   const int64_t row_tiles = (ea.B + NW * RW - 1) / (NW * RW);
-  if (row_tiles * ea.n_tiles > 0x7fffffffLL) return fail(LUTKAN_EUNSUPPORTED, "bspline_tiled_kernel: B * m too large for one launch");
+  if (!lutkan::launch_holds(row_tiles * ea.n_tiles, kTileWaves * 64)) return fail(LUTKAN_EUNSUPPORTED, "bspline_tiled_kernel: B * m too large for one launch");
   const dim3 grid((unsigned)(row_tiles * ea.n_tiles), (unsigned)((ea.d + ea.chunk - 1) / ea.chunk));
   const size_t lds = 2 * (size_t)bytes + (size_t)NW * 2 * RW * 32;
   static LdsCap raised, raised_base;
@@ -414,6 +414,7 @@ int bspline_impl(const bspline_dev_layer *l, const float *x, int64_t B, float *y
     const int cols = ((l->d + 15) / 16 * 16 < (l->d + 31) / 32 * 32) ? 16 : 32;      // the width that pads d least
     const dim3 lgrid((unsigned)(Bp / (kSplTile / cols)), (unsigned)((l->d + cols - 1) / cols));
     if (lgrid.y > 65535u) return fail(LUTKAN_EUNSUPPORTED, "%s: d too large", who);
+    if (!lutkan::launch_holds(Bp / (kSplTile / cols), 256)) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large for one launch", who);
     if (l->knots_per_input) {
       if (cols == 32) hipLaunchKernelGGL((bspline_locate_kernel<32, true>), lgrid, dim3(256), 0, s, la);
       else hipLaunchKernelGGL((bspline_locate_kernel<16, true>), lgrid, dim3(256), 0, s, la);
@@ -457,7 +458,9 @@ int bspline_impl(const bspline_dev_layer *l, const float *x, int64_t B, float *y
   float *partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + record_bytes(l->d, Bp, 32));
   ea.chunk = gp.chunk;
   if (gp.n_split > 1) { ea.y = partials; ea.split_stride = B * l->m; }
-  const dim3 grid((unsigned)((B + (256 >> lg) - 1) / (256 >> lg)), (unsigned)((l->m + (1 << lg) - 1) >> lg), (unsigned)gp.n_split);
+  const int64_t row_groups = (B + (256 >> lg) - 1) / (256 >> lg);
+  if (!lutkan::launch_holds(row_groups, 256)) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large for one launch", who);
+  const dim3 grid((unsigned)row_groups, (unsigned)((l->m + (1 << lg) - 1) >> lg), (unsigned)gp.n_split);
   hipLaunchKernelGGL(bspline_gather_kernel, grid, dim3(256), 0, s, ea, lg);
   if (int rc = check_launch("bspline_gather_kernel")) return rc;
   lutkan::plan_note("bspline_gather split=%d; ", gp.n_split);

@@ -474,7 +474,7 @@ template <int GRP, int RT, int NT>
 int launch_matrix(const SplineMatrixArgs &ma, int n_split, hipStream_t s) {
   constexpr int kRows = kMxWaves * 32 * RT;
   const int64_t groups = (ma.B + kRows - 1) / kRows * ma.n_tiles;
-  if (groups > 0x7fffffffLL) return fail(LUTKAN_EUNSUPPORTED, "bspline_matrix_kernel: B * m too large for one launch");
+  if (!lutkan::launch_holds(groups, kMxWaves * 64)) return fail(LUTKAN_EUNSUPPORTED, "bspline_matrix_kernel: B * m too large for one launch");
   const size_t lds = 2 * (size_t)((GRP == 3 ? 12 : 8) * 3 * 32 * NT * 16) + kMxLdsTail;
   static LdsCap raised;
   if (int rc = raise_lds_cap(bspline_matrix_kernel<GRP, RT, NT>, &raised, "bspline_matrix_kernel")) return rc;

@@ -173,11 +173,11 @@ inline int32_t padded_columns(int32_t m) { return (m + kBN - 1) / kBN * kBN; }
 
 namespace lutkan {
 
-// A launch holds fewer than 2^32 threads.  Batches beyond 65535 row tiles leave the base branch in the edge kernel: it serves them as fast
+// Batches beyond 65535 row tiles leave the base branch in the edge kernel: it serves them as fast
 // or faster (32 -> 64 at 8388865 rows 4.09 ms against 5.02 by the product, 64 -> 128 12.07 against 12.08).
 bool base_product_fits(int32_t d, int32_t m, int64_t B) {
   const int64_t row_tiles = (B + kBM - 1) / kBM;
-  return d % kBK == 0 && m >= 64 && row_tiles <= 65535 && row_tiles * (padded_columns(m) / kBN) * (kGemmWaves * 64) <= 0xffffffffLL;
+  return d % kBK == 0 && m >= 64 && row_tiles <= 65535 && launch_holds(row_tiles * (padded_columns(m) / kBN), kGemmWaves * 64);
 }
 
 size_t base_product_workspace_bytes(int32_t d, int32_t m) {

@@ -154,9 +154,6 @@ inline bool overlap(const float *x, int64_t n_x, const float *y, int64_t n_y) {
   return LUTKAN_OK;
 }
 
-// A launch holds fewer than 2^32 threads: of more the count is cut to 32 bits, and no error says so.
-constexpr int64_t kMaxLaunchThreads = 0xffffffffLL;
-
 enum { kLocate = 1, kEdges = 2 };      // the two phases of a forward call
 
 inline int gather_jx_log2(int m) {

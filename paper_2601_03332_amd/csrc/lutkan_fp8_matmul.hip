@@ -699,7 +699,7 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   }
   if (tiles(16) > 65535) price[kDirect16x16] = price[kDirect16x32] = HUGE_VAL;
   if (tiles(32) > 65535) price[kDirect32x32] = HUGE_VAL;
-  const auto beyond_a_launch = [&](int side, int threads) { return tiles(side) * ((a.n + side - 1) / side) > kMaxLaunchThreads / threads; };
+  const auto beyond_a_launch = [&](int side, int threads) { return !lutkan::launch_holds(tiles(side) * ((a.n + side - 1) / side), threads); };
   if (beyond_a_launch(64, 1024)) price[kTiled64x4] = HUGE_VAL;
   if (beyond_a_launch(64, 512)) price[kTiled64x2] = HUGE_VAL;
   if (beyond_a_launch(128, 512)) price[kTiled128x2] = HUGE_VAL;

@@ -250,7 +250,7 @@ extern "C" int lutkan_rmsnorm_fp8(const lutkan_rmsnorm_fp8_args *p, void *hip_st
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const unsigned threads = waves == 1 ? 64u * kRowsOfGroup : (unsigned)waves * 64u;
   const int group_rows = waves == 1 ? kRowsOfGroup : 1;
-  const int64_t launch_rows = kMaxLaunchThreads / threads * group_rows;          // (more rows: more launches)
+  const int64_t launch_rows = lutkan::kMaxLaunchThreads / threads * group_rows;          // (more rows: more launches)
   const int64_t residual_bytes = p->residual ? type_bytes(p->residual_type) : 0;
   for (int64_t first = 0; first < p->rows; first += launch_rows) {
     NormArgs a;
@@ -287,7 +287,7 @@ extern "C" int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t mat
   a.w_stride = stride; a.w_matrix_stride = matrix_stride; a.n = n; a.k = k;
   const int64_t per_matrix = scale_blocks(n) * scale_blocks(k);
   if (matrices > 0x7fffffff / per_matrix) return fail(LUTKAN_EUNSUPPORTED, "%s: too many blocks", who);
-  const int64_t all = matrices * per_matrix, launch_blocks = kMaxLaunchThreads / 256;      // (more blocks: more launches)
+  const int64_t all = matrices * per_matrix, launch_blocks = lutkan::kMaxLaunchThreads / 256;      // (more blocks: more launches)
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   for (int64_t first = 0; first < all; first += launch_blocks) {
     a.first = (unsigned)first;

@@ -49,6 +49,9 @@ inline int coef_slice_rows(int R, int value_repr) { return R + (value_repr == LU
 
 // LDS that one work-group of the tiled kernels may use: all 160 KiB of a gfx950 compute unit.
 constexpr int kLdsPerWorkGroup = 160 * 1024;
+// A launch holds fewer than 2^32 threads: of more the count is cut to 32 bits, and no error says so.
+constexpr int64_t kMaxLaunchThreads = 0xffffffffLL;
+inline bool launch_holds(int64_t groups, int threads) { return groups <= kMaxLaunchThreads / threads; }
 
 // Largest table slice of the LUT tiled kernel: two slice buffers plus the per-wave record buffers (16 waves x 2 buffers
 // x at most 64 rows of 8-byte records, 16-byte with the base branch) must fit: 72 KiB, 64 KiB with the base branch.

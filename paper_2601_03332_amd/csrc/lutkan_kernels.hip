@@ -1013,7 +1013,7 @@ int launch_tiled_np(const EdgeArgs &ea, hipStream_t s) {
   constexpr int NW = kTileWaves;
   constexpr int RW = (64 / LPR) * NP;
   const int64_t row_tiles = (ea.B + NW * RW - 1) / (NW * RW);
-  if (row_tiles * ea.n_tiles > 0x7fffffffLL) return fail(LUTKAN_EUNSUPPORTED, "lutkan_tiled_kernel: B * m too large for one launch");
+  if (!lutkan::launch_holds(row_tiles * ea.n_tiles, kTileWaves * 64)) return fail(LUTKAN_EUNSUPPORTED, "lutkan_tiled_kernel: B * m too large for one launch");
   const dim3 grid((unsigned)(row_tiles * ea.n_tiles), (unsigned)((ea.d + ea.chunk - 1) / ea.chunk));
   const int pipe = tiled_pipe(ea, NP);
   const size_t lds = (pipe == 2) ? 2 * (size_t)ea.blob_bytes + (size_t)NW * 2 * RW * (ea.with_base ? 16 : 8)
@@ -1098,6 +1098,7 @@ int launch_locate(hipStream_t s, const LocateArgs &la, const char *who) {
   const unsigned col_tiles = (unsigned)((la.d + cols - 1) / cols);
   if (col_tiles > 65535u) return fail(LUTKAN_EUNSUPPORTED, "%s: d too large", who);
   const int64_t row_tiles = (la.Bp + 2048 / cols - 1) / (2048 / cols);
+  if (!lutkan::launch_holds(row_tiles, 256)) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large for one launch", who);
   if (row_tiles * col_tiles >= 512) launch_locate_tile<BASE, PERIN, 8>(cols, dim3((unsigned)row_tiles, col_tiles), s, la);
   else launch_locate_tile<BASE, PERIN, 2>(cols, dim3((unsigned)((la.Bp + 512 / cols - 1) / (512 / cols)), col_tiles), s, la);
   return check_launch("lutkan_locate_kernel");
@@ -1141,7 +1142,7 @@ int chain_impl(const lutkan_dev_layer *layers, int32_t n_layers, const float *x,
   const int wpr = (B <= kChainSplitRows) ? kChainWaves : 1;
   const int rows_per_group = kChainWaves / wpr;
   const int64_t groups = (B + rows_per_group - 1) / rows_per_group;
-  if (groups > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large", who);
+  if (!lutkan::launch_holds(groups, kChainWaves * 64)) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large", who);
   ca.x = x; ca.y = y; ca.hidden = hidden;
   ca.stats = reinterpret_cast<unsigned long long *>(stats);
   ca.B = B; ca.n_layers = n_layers; ca.rec_stride = widest;
@@ -1189,6 +1190,7 @@ bool small_layer_runs_as_chain(const lutkan_dev_layer *l, int64_t B) {
 // The OOB counters of a layer's inputs, added to `stats`.
 int count_oob(const lutkan_dev_layer *l, const float *x, int64_t B, lutkan_oob_stats *stats, hipStream_t s) {
   const int64_t rows_per_group = 4 * kOobRowsPerWave;
+  if (!lutkan::launch_holds((B + rows_per_group - 1) / rows_per_group, 256)) return fail(LUTKAN_EUNSUPPORTED, "oob_count_kernel: B too large for one launch");
   hipLaunchKernelGGL(oob_count_kernel, dim3((unsigned)((B + rows_per_group - 1) / rows_per_group)), dim3(256), 0, s, x, B, l->d,
                      l->knots[0], l->knots[l->K], l->boundary == LUTKAN_CLOSED ? 1 : 0, l->knots_per_input ? l->input_knots : nullptr, l->K,
                      reinterpret_cast<unsigned long long *>(stats));
@@ -1385,7 +1387,9 @@ int forward_impl(const lutkan_dev_layer *l, const float *x, int64_t B, float *y,
     ea.chunk = gp.chunk;
     if (gp.n_split > 1) { ea.y = partials; ea.split_stride = B * l->m; }
     const int rows_per_group = 256 >> lpr_log2;
-    const dim3 grid((unsigned)((B + rows_per_group - 1) / rows_per_group), (unsigned)l->n_tiles, (unsigned)gp.n_split);
+    const int64_t row_groups = (B + rows_per_group - 1) / rows_per_group;
+    if (!lutkan::launch_holds(row_groups, 256)) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large for one launch", who);
+    const dim3 grid((unsigned)row_groups, (unsigned)l->n_tiles, (unsigned)gp.n_split);
     if (grid.y > 65535u) return fail(LUTKAN_EUNSUPPORTED, "%s: m too large for the gather kernel", who);
     const bool sym = (l->scheme == LUTKAN_SYM_INT8);
 #define LUTKAN_LAUNCH_GATHER4(S, BASE, PH) hipLaunchKernelGGL((lutkan_gather4_kernel<S, BASE, PH, kGather4Inputs>), grid, dim3(256), 0, s, ea, lpr_log2)
@@ -1406,7 +1410,9 @@ int forward_impl(const lutkan_dev_layer *l, const float *x, int64_t B, float *y,
   const GatherPlan gp = plan_gather(B, l->d, l->m);
   ea.chunk = gp.chunk;
   if (gp.n_split > 1) { ea.y = partials; ea.split_stride = B * l->m; }
-  const dim3 grid((unsigned)((B + (256 >> lg) - 1) / (256 >> lg)), (unsigned)((l->m + (1 << lg) - 1) >> lg), (unsigned)gp.n_split);
+  const int64_t row_groups = (B + (256 >> lg) - 1) / (256 >> lg);
+  if (!lutkan::launch_holds(row_groups, 256)) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large for one launch", who);
+  const dim3 grid((unsigned)row_groups, (unsigned)((l->m + (1 << lg) - 1) >> lg), (unsigned)gp.n_split);
   if (grid.y > 65535u) return fail(LUTKAN_EUNSUPPORTED, "%s: m too large for the gather kernel", who);
   if (l->scheme == LUTKAN_SYM_INT8) {
     if (q01_out) hipLaunchKernelGGL((lutkan_gather_kernel<LUTKAN_SYM_INT8, true>), grid, dim3(256), 0, s, ea, lg);
@@ -1504,7 +1510,7 @@ extern "C" int lutkan_wide_table_build(lutkan_dev_layer *layer, int32_t code_byt
   if (!need) return fail(LUTKAN_EUNSUPPORTED, "%s: the layer has no wide form of %d bytes per code (64-column tiles whose wide slice fits the LDS twice; jt = %d, K*L = %d)", who, code_bytes, layer->jt, layer->K * layer->L);
   if (!wide_table || (reinterpret_cast<uintptr_t>(wide_table) & 15) != 0) return fail(LUTKAN_EINVAL, "%s: wide_table must be a 16-byte aligned device pointer", who);
   if (bytes < need) return fail(LUTKAN_ESHAPE, "%s: %zu bytes, need %zu", who, bytes, need);
-  if ((int64_t)layer->n_tiles * layer->d > 0x7fffffffLL) return fail(LUTKAN_EUNSUPPORTED, "%s: too many slices", who);
+  if (!lutkan::launch_holds((int64_t)layer->n_tiles * layer->d, 256)) return fail(LUTKAN_EUNSUPPORTED, "%s: too many slices", who);
   const lutkan::BlobLayout lay = lutkan::blob_layout(layer->K, layer->L, layer->jt, layer->scheme, layer->value_repr, layer->param_dtype);
   WidenArgs a;
   a.src = static_cast<const unsigned char *>(layer->table);

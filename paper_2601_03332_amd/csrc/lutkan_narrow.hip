@@ -240,7 +240,7 @@ template <int SCHEME, int LPR, int S, int NW>
 int launch_narrow(const NarrowArgs &na, bool base, bool half_params, int n_split, hipStream_t s) {
   constexpr int kRows = NW * (64 / LPR);
   const int64_t groups = (na.B + kRows - 1) / kRows;
-  if (groups > 0x7fffffffLL) return fail(LUTKAN_EUNSUPPORTED, "lutkan_narrow_kernel: B too large for one launch");
+  if (!lutkan::launch_holds(groups, NW * 64)) return fail(LUTKAN_EUNSUPPORTED, "lutkan_narrow_kernel: B too large for one launch");
   const dim3 grid((unsigned)groups, (unsigned)n_split);
   const size_t lds = narrow_lds_bytes(S, na.blob_bytes, na.K);
 #define LUTKAN_LAUNCH_NARROW(BASE, PH)                                                                                            \

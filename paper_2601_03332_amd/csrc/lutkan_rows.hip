@@ -189,7 +189,7 @@ int rows_depth(int64_t B, int n_tiles, int jt, int wpr, int d) {
 template <int SCHEME, int LPR, int WPR, int DEPTH>
 int launch_rows_kernel(const RowsArgs &ra, hipStream_t s) {
   const int64_t groups = rows_groups(ra.B, WPR, ra.n_tiles);
-  if (groups > 0x7fffffffLL) return fail(LUTKAN_EUNSUPPORTED, "lutkan_rows_kernel: B * m too large for one launch");
+  if (!lutkan::launch_holds(groups, kRowsWaves * 64)) return fail(LUTKAN_EUNSUPPORTED, "lutkan_rows_kernel: B * m too large for one launch");
   const size_t lds = rows_lds(4 * LPR, WPR, ra.d);
   static LdsCap raised;
   if (int rc = raise_lds_cap(lutkan_rows_kernel<SCHEME, LPR, WPR, DEPTH>, &raised, "lutkan_rows_kernel")) return rc;

@@ -167,7 +167,7 @@ extern "C" int lutkan_error_stats(const float *y, const float *y_ref, int64_t B,
   if (!workspace || workspace_bytes < need) return fail(LUTKAN_ESHAPE, "%s: workspace of %zu bytes, need %zu", who, workspace_bytes, need);
   if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return fail(LUTKAN_EINVAL, "%s: workspace must be 16-byte aligned", who);
   const int64_t groups = stat_groups(B);
-  if (groups > 0x7fffffff) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large", who);
+  if (!lutkan::launch_holds(groups, kStatWaves * 64)) return fail(LUTKAN_EUNSUPPORTED, "%s: B too large", who);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   Partial *partials = static_cast<Partial *>(workspace);
   hipLaunchKernelGGL(error_stats_partial_kernel, dim3((unsigned)groups), dim3(kStatWaves * 64), 0, s, y, y_ref, x, B, m, d, t0, tK,
