@@ -426,7 +426,8 @@ int lutkan_quantise_fp8(const void *weight, int32_t type, int64_t matrices, int3
                         void *codes, float *scales, void *hip_stream);
 
 /* y[s][j] = sum over blocks b of x_scales[s][b] * weight_scales[j / 128][b] * (sum over k in b of x[s][k] * weight[j][k]).
- * A block's products are summed on the matrix cores, the blocks in fp32; y is rounded once, to y_type.  The order of the sum
+ * A block's products are summed on the matrix cores, the blocks in fp32 (a row with a block whose scales are finite and their product is
+ * not in fp64, if an output would not be finite else); y is rounded once, to y_type.  The order of the sum
  * over blocks depends on the sizes, not on the run: equal calls give equal bits.
  * lutkan_matmul_fp8 takes one weight; rows == x_rows, and the fields from group_sizes on are not read.
  * lutkan_grouped_matmul_fp8 takes `groups` weights: rows of y in groups, one after the other, group g the next group_sizes[g]

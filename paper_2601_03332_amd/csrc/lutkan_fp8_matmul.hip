@@ -241,6 +241,52 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs &a, int64_t row)
   return row;
 }
 
+// Outputs that are not finite, once more.  Both scales meet before the block's sum: where their product passes fp32's range though each is
+// finite, a sum of zero comes out as NaN and a small one as infinite.  Rows of the tile with such a block are computed again in
+// fp64, an output to a lane, by the wave that stored them; other rows stay as they are.  (The kernels' loops have no place to look for
+// it; this costs them one multiply-add an output.)
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+template <int ROWS, int COLS, bool GROUPED>
+__device__ __forceinline__ void again_in_fp64(const RowTile &t, int64_t row0, int col0) {
+  static_assert(kScaleBlock % COLS == 0, "columns of one block");
+  uintptr_t args = (uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();      // the arguments anew: kept until here they would take scalar registers throughout
+  asm volatile("" : "+s"(args));
+  const ProductArgs a = *reinterpret_cast<const ProductArgs *>(args);
+  const int lane = threadIdx.x & 63, k_blocks = a.k_blocks();
+  const float *ws = a.w_scales + ((int64_t)t.group * a.n_blocks() + col0 / kScaleBlock) * k_blocks;
+  wait_all_vector_loads();                                       // (and stores: what is written here comes behind them)
+#pragma unroll 1
+  for (int part = 0; part < ROWS; part += 64) {
+    bool beyond = false;
+    const int64_t own = row0 + part + lane;
+    if (part + lane < ROWS && own < t.end) {
+      const int64_t from = source_row<GROUPED>(a, own);
+      const float *xs = a.x_scales + max(from, (int64_t)0) * a.x_scales_stride;
+      for (int b = 0; from >= 0 && b < k_blocks; ++b) beyond |= finite(xs[b]) && finite(ws[b]) && !finite(xs[b] * ws[b]);
+    }
+    for (unsigned long long rows = __ballot(beyond); rows != 0; rows &= rows - 1) {
+      const int64_t row = row0 + part + __builtin_ctzll(rows), from = source_row<GROUPED>(a, row);
+      const int col = col0 + lane;
+      if (lane >= COLS || col >= a.n) continue;
+      const unsigned char *x = a.x + from * a.x_stride, *w = a.w + t.group * a.w_matrix_stride + (int64_t)col * a.w_stride;
+      const float *xs = a.x_scales + from * a.x_scales_stride;
+      double sum = 0.0;
+#pragma unroll 1
+      for (int b = 0; b < k_blocks; ++b) {
+        double of_block = 0.0;
+#pragma unroll 1
+        for (int k = b * kScaleBlock; k < min(a.k, (b + 1) * kScaleBlock); ++k)
+          of_block += (double)(__builtin_amdgcn_cvt_f32_fp8(x[k], 0) * __builtin_amdgcn_cvt_f32_fp8(w[k], 0));
+        sum += (double)xs[b] * (double)ws[b] * of_block;
+      }
+      unsigned char *to = a.y + (row * a.y_stride + col) * type_bytes(a.y_type);
+      if (a.y_type == LUTKAN_F32) store_one<LUTKAN_F32>(to, (float)sum);
+      else if (a.y_type == LUTKAN_F16) store_one<LUTKAN_F16>(to, (float)sum);
+      else store_one<LUTKAN_BF16>(to, (float)sum);
+    }
+  }
+}
+
 // A work-group computes 16 MT rows x 16 NT columns from global memory straight into registers; its waves take the blocks of k in turn,
 // and their sums meet in LDS in the waves' order.
 // Bound by what it reads, as no work-group shares with another: 16 rows of 4096 -> 4096 7.2 us a call (16 x 16: 256 work-groups, one to a
@@ -351,6 +397,7 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
       for (int n = 0; n < NT; ++n) s_part[((wave * MT + m) * NT + n) * 64 + lane] = acc[m][n];
     __syncthreads();
   }
+  unsigned again = 0;                                            // tiles with outputs that are not finite
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -364,7 +411,12 @@ __global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_k
       if (none[m]) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       const int64_t row = t.first + 16 * m + (lane & 15);
       if (row < t.end) store_outputs(a, row, col0 + 16 * n + 4 * p, v);
+      if (__any(!(finite(v.x) && finite(v.y) && finite(v.z) && finite(v.w)))) again |= 1u << (m * NT + n);
     }
+  for (; again != 0; again &= again - 1) {
+    const int tile = __builtin_ctz(again);
+    again_in_fp64<16, 16, GROUPED>(t, t.first + 16 * (tile / NT), col0 + 16 * (tile % NT));
+  }
 }
 
 template <int MT, int NT, bool EXACT, bool GROUPED>
@@ -602,14 +654,20 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
     }
   }
   if (KG > 1 && team > 0) return;
+  f32x4 seen{0.0f, 0.0f, 0.0f, 0.0f};                            // NaN once an output is not finite
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int64_t row = t.first + (wm * MT + m) * 16 + (lane & 15);
     const bool none = t.group < 0 || (GROUPED && row < t.end && source_row<GROUPED>(a, row) < 0);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[m][n] = none ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[m][n];
+    for (int n = 0; n < NT; ++n) {
+      acc[m][n] = none ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[m][n];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) seen[e] = fmaf(acc[m][n][e], 0.0f, seen[e]);
+    }
     store_row<NT>(a, row, row < t.end, col0 + wn * NT * 16, p, acc[m]);
   }
+  if (__any((seen[0] + seen[1]) + (seen[2] + seen[3]) != 0.0f)) again_in_fp64<16 * MT, 16 * NT, GROUPED>(t, t.first + wm * MT * 16, col0 + wn * NT * 16);
 }
 
 template <int MT, int NT, int WM, int WN, int KG, bool EXACT, bool GROUPED, bool ASYNC>

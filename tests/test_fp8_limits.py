@@ -145,3 +145,60 @@ def test_the_block_refuses_a_router_that_does_not_fit_its_experts():
             ExpertBlock(norm, torch.zeros(shape), torch.zeros(4, 6, 10), layer)
     with pytest.raises(lk.LutKanError, match="experts are"):
         ExpertBlock(norm, torch.zeros(4, 10), torch.zeros(6, 10), layer)
+
+
+# ---------------------------------------------------------------- scales whose product is out of range
+@gpu
+@pytest.mark.parametrize("case", [(False, 1, 300, 40, 0), (True, 1, 300, 40, 0), (False, 33, 301, 50, 3), (True, 70, 300, 260, 0), (False, 2449, 617, 194, 0), (True, 2502, 1028, 293, 0),
+                                  (False, 3489, 264, 3001, 0), (False, 2846, 3108, 835, 5), (True, 3642, 1345, 531, 0), (True, 3979, 236, 870, 5)], ids=str)
+def test_scales_whose_product_is_beyond_the_type(case):
+    """scale(x) * scale(w) beyond 2^128 with both finite: a block whose sum is zero adds nothing, one whose sum is small adds what it comes to;
+    infinite scales and NaN codes stay what they are."""
+    wide, rows, k, n, groups = case
+    print(f"case scales {case}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(k)
+    blocks, lead = -(-k // 128), [groups] if groups else []
+    ones = torch.tensor([0x38, 0xb8], dtype=torch.uint8, device=DEV)
+
+    def signs(*shape):
+        return ones[torch.randint(0, 2, shape, generator=gen, device=DEV)]
+    x, w = signs(rows, k), signs(*lead, n, k)
+    xs, ws = torch.ones(rows, blocks, device=DEV), torch.ones(*lead, -(-n // 128), blocks, device=DEV)
+    ws[..., 0] = 2.0 ** 60
+    every = torch.arange(rows, device=DEV)
+    xs[every % 3 == 0, 0] = 2.0 ** 100                             # times 2^60: beyond the type.  Codes of zero in every other of these rows,
+    x[every % 3 == 0, :128] = 0
+    x[every % 6 == 3, 5] = 0x01                                    # 2^-9, the smallest code, in the others, whose scale is 2^70: 2^121
+    xs[every % 6 == 3, 0] = 2.0 ** 70
+    sizes = [rows // 2, rows - rows // 2] + [0] * (groups - 2) if groups else [rows]
+    xd, wd = (torch.where((c & 0x80) != 0, -1.0, 1.0).double() * torch.where((c & 0x7f) == 1, 2.0 ** -9, torch.where((c & 0x7f) == 0, 0.0, 1.0)).double() for c in (x, w))
+    ref, first = torch.zeros(rows, n, dtype=torch.float64, device=DEV), 0
+    for e, size in enumerate(sizes):
+        at = slice(first, first + size)
+        ws_e, wd_e = (ws[e], wd[e]) if groups else (ws, wd)
+        sw = ws_e.double().repeat_interleave(128, 0)[:n].repeat_interleave(128, 1)[:, :k]
+        ref[at] = (xd[at] * xs[at].double().repeat_interleave(128, 1)[:, :k]) @ (wd_e * sw).t().contiguous()
+        first += size
+    for dtype in [torch.float32] if wide else [torch.bfloat16]:
+        def call():
+            if groups:
+                return lk.lutkan_grouped_matmul_fp8(x.view(F8), xs, w.view(F8), ws, torch.tensor(sizes, device=DEV), dtype=dtype)
+            return lk.lutkan_matmul_fp8(x.view(F8), xs, w.view(F8), ws, dtype=dtype)
+        y = call()
+        assert bool(torch.isfinite(y).all())
+        # rows of zeros in the first block: whole numbers below 2^13, exact before the output's rounding; the others: 2^121 times what fp32 rounds
+        zero = every % 6 == 0
+        assert torch.equal(y[zero], ref[zero].float().to(dtype))
+        other = every % 6 == 3
+        assert bool(((y[other].double() - ref[other]).abs() <= (2.0 ** -22 if wide else 2.0 ** -7) * ref[other].abs()).all())
+        rest = every % 3 != 0                                      # first block 2^60 times a whole number: the rest is below its last bit
+        assert bool(((y[rest].double() - ref[rest]).abs() <= (2.0 ** -22 if wide else 2.0 ** -7) * ref[rest].abs() + 2.0 ** 14).all())
+        kept = xs[0, 0].item()
+        xs[0, 0] = float("inf")
+        got = call()
+        assert not bool(torch.isfinite(got[0]).any()) and torch.equal(got[1:], y[1:])
+        xs[0, 0] = kept
+        x[0, k - 1] = 0x7f
+        got = call()
+        assert bool(torch.isnan(got[0]).all()) and torch.equal(got[1:], y[1:])
+        x[0, k - 1] = 0x38
