@@ -445,7 +445,13 @@ __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ 
 // As copy16_global_to_lds_at, four bytes a lane.
 __device__ __forceinline__ void copy4_global_to_lds_at(const void *uniform_base, unsigned lane_byte_offset, void *lds_dst) {
   const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)lds_dst);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(lane_byte_offset), "s"(uniform_base) : "m0", "memory");
+  if constexpr (kLdsDmaPreservesM0) {
+    unsigned saved;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved) : "s"(dst), "v"(lane_byte_offset), "s"(uniform_base) : "memory");
+  } else {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(lane_byte_offset), "s"(uniform_base) : "m0", "memory");
+  }
 }
 
 // The sizes of a tile, its buffers and its team.

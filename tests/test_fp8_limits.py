@@ -202,3 +202,37 @@ def test_scales_whose_product_is_beyond_the_type(case):
         got = call()
         assert bool(torch.isnan(got[0]).all()) and torch.equal(got[1:], y[1:])
         x[0, k - 1] = 0x38
+
+
+# ---------------------------------------------------------------- the copies into LDS
+def test_every_copy_into_lds_preserves_m0_where_that_is_switched_on(tmp_path):
+    """kLdsDmaPreservesM0 is for a compiler that keeps values in M0: with it, every copy in the products' kernels saves M0 and puts it back."""
+    import os
+    import re
+    import shutil
+    import subprocess
+    from paper_2601_03332_amd import build as lib_build
+    for name in os.listdir(lib_build.CSRC):
+        if name.endswith(".h") or name == "lutkan_fp8_matmul.hip":
+            shutil.copy(os.path.join(lib_build.CSRC, name), tmp_path / name)
+    header = (tmp_path / "lutkan_device.h").read_text()
+    assert header.count("kLdsDmaPreservesM0 = false") == 1
+    (tmp_path / "lutkan_device.h").write_text(header.replace("kLdsDmaPreservesM0 = false", "kLdsDmaPreservesM0 = true"))
+    out = tmp_path / "matmul.s"
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")] + lib_build.HIPCC_FLAGS +
+                   ["-I", os.path.join(lib_build.ROOT, "include"), "-I", str(tmp_path), "-x", "hip", "--cuda-device-only", "-S", str(tmp_path / "lutkan_fp8_matmul.hip"), "-o", str(out)],
+                   check=True, capture_output=True)
+    copies = {"global_load_lds_dword": 0, "global_load_lds_dwordx4": 0}
+    block = []
+    for line in open(out):
+        text = line.strip()
+        if text.startswith(";;#ASMSTART"):
+            block = []
+        elif text.startswith(";;#ASMEND"):
+            for load in (t.split()[0] for t in block if t.startswith("global_load_lds")):
+                copies[load] += 1
+                saved = re.fullmatch(r"s_mov_b32 (s\d+), m0", block[0])
+                assert saved and block[-1] == f"s_mov_b32 m0, {saved.group(1)}", block
+        else:
+            block.append(text.split(";")[0].strip())
+    assert min(copies.values()) > 0
