@@ -888,7 +888,8 @@ def _matmul_fp8(who, x, x_scales, weight, weight_scales, y, dtype, rows, experts
 def lutkan_matmul_fp8(x, x_scales, weight, weight_scales, y=None, dtype=None):
     """y [rows, n] = x [rows, k] times weight [n, k] transposed, both as codes (float8_e4m3fn) with their scales (of lutkan_rmsnorm_fp8
     and lutkan_quantise_fp8, or a checkpoint's in that layout), on the current stream.  dtype: of y where none is given (float32, which
-    a layer takes, is the default; float16, bfloat16)."""
+    a layer takes, is the default; float16, bfloat16).  The type of y also chooses how a block of 128 is summed: in fp32 for float32, with the
+    8-bit matrix instruction, at twice the rate and with 13 bits below the largest of eight products, for the 16-bit types (see lutkan.h)."""
     who, torch = "lutkan_matmul_fp8", _torch()
     dtype = torch.float32 if dtype is None else dtype
     if y is None:

@@ -85,8 +85,9 @@ __device__ __forceinline__ float block_scale(unsigned largest) {
 }
 
 // Eight codes of v / scale, rounded to nearest, ties to even.  The quotient is v * inverse corrected by its own remainder, so that it is
-// rounded once: v * inverse alone can fall on the other side of a tie.  |v| <= 448 scale, so it is at most 448;
-// infinities and NaN only come with a scale that is not finite either, and then every code is NaN or stands for it.
+// rounded once: v * inverse alone can fall on the other side of a tie.  A scale that was rounded down lets it pass 448 by 2^-24 of it,
+// which the conversion rounds back.  Infinities and NaN only come with a scale that is not finite either, and then every code is NaN or
+// stands for it.
 __device__ __forceinline__ float quotient(float v, float scale, float inverse) {
   const float q = v * inverse;
   return fmaf(fmaf(-q, scale, v), inverse, q);

@@ -8,7 +8,8 @@
 // the result for normally distributed inputs, 1/100 of what the rounding to bf16 costs and 1/20 of that to f16.  Outputs of 16 bits are
 // computed with it.  Outputs of 32 bits would lose by it what their type could hold, so for them every code is converted to bf16,
 // which holds all of its values, and the product taken with the 16-bit instruction (16 x 16 x 32, four for a block, half the rate),
-// whose sums are good to 2^-24.
+// whose sums are good to 2^-24.  Where a block's large products cancel, what the 8-bit instruction cuts is a part of them and not of their sum
+// (at most 2^-10 of the sum of magnitudes): callers who need that ask for 32 bits.
 //
 // The weight is the instruction's first operand and the activations its second, so that a lane holds four neighbouring outputs of one
 // row: one activation scale per lane, and outputs that are stored as a vector.  Both operands are read in the same order along k (a
@@ -292,7 +293,7 @@ __device__ __forceinline__ void again_in_fp64(const RowTile &t, int64_t row0, in
 // Bound by what it reads, as no work-group shares with another: 16 rows of 4096 -> 4096 7.2 us a call (16 x 16: 256 work-groups, one to a
 // compute unit, weights 17 MB and as much of x again; 9.0 with 16 x 32); one row 5.3.
 template <int MT, int NT, bool EXACT, bool GROUPED, bool ALIGNED>
-__global__ __launch_bounds__(MT * NT <= 4 ? 1024 : 512) void lutkan_fp8_direct_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(1024) void lutkan_fp8_direct_kernel(const ProductArgs a) {
   extern __shared__ __align__(16) f32x4 s_part[];                // [wave][row tile][column tile][lane]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = a.extent;
   const int p = lane >> 4, col0 = blockIdx.x * (16 * NT);

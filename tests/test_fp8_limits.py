@@ -134,6 +134,31 @@ def test_the_most_groups():
     assert torch.equal(y, expected)
 
 
+# ---------------------------------------------------------------- large products that cancel
+@gpu
+@pytest.mark.parametrize("shape", [(5, 384, 40), (3000, 384, 2048)], ids=str)
+def test_large_products_that_cancel(shape):
+    """448 * 448 and its negative side by side, and products of at most 1 among them.  Outputs of 32 bits: a sum of a block is off by at most
+    2^-23 of its largest partial sum, 448^2, per addition (128, and 3 blocks): 131 * 2^-23 * 448^2 = 3.2.  Those of 16 bits keep 13 bits below the
+    leading bit of 448^2: seven products in a group of eight, 16 groups, 3 blocks, 2^17 * 2^-13 each, and the output's rounding."""
+    rows, k, n = shape
+    print(f"case cancel {shape}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(k)
+    codes = torch.tensor([0x00, 0x30, 0x38, 0xb0, 0xb8], dtype=torch.uint8, device=DEV)        # 0, 1/2, 1, -1/2, -1
+    x, w = (codes[torch.randint(0, 5, (count, k), generator=gen, device=DEV)] for count in (rows, n))
+    large = torch.randperm(k // 2, generator=gen, device=DEV)[:k // 16] * 2
+    x[:, large], x[:, large + 1], w[:, large], w[:, large + 1] = 0x7e, 0xfe, 0x7e, 0x7e        # 448, -448; 448, 448
+    value = torch.zeros(256, dtype=torch.float64, device=DEV)
+    value[[0x30, 0x38, 0xb0, 0xb8]] = torch.tensor([0.5, 1, -0.5, -1], dtype=torch.float64, device=DEV)
+    ref = value[x.long()] @ value[w.long()].t().contiguous()       # (the large ones add to 0 exactly)
+    xs, ws = torch.ones(rows, k // 128, device=DEV), torch.ones(-(-n // 128), k // 128, device=DEV)
+    for dtype, bound in ((torch.float32, 3.2), (torch.float16, 7 * 16 * 3 * 16.0), (torch.bfloat16, 7 * 16 * 3 * 16.0)):
+        y = lk.lutkan_matmul_fp8(x.view(F8), xs, w.view(F8), ws, dtype=dtype)
+        off = float((y.double() - ref).abs().max())
+        print(f"{dtype}: {off} of values to {float(ref.abs().max())}", flush=True)
+        assert off <= bound
+
+
 # ---------------------------------------------------------------- the block
 def test_the_block_refuses_a_router_that_does_not_fit_its_experts():
     """A router of more rows than there are experts would pick experts that do not exist."""
