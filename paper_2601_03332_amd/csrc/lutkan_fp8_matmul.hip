@@ -437,10 +437,11 @@ int launch_direct(ProductArgs a, int64_t row_tiles, bool aligned, const char *wh
 // lie in different banks (no conflict counted).
 //   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and
 //   offsets that fit 32 bits.  Otherwise, and for a last block that is not whole, through registers.
-// What it measured, into bf16, 8192 rows of 4096 -> 4096: 256 x 256 outputs 119 - 124 us on the same inputs again and again, 127 - 137 on three sets
-// in turn (2.3 - 2.0 PFLOP/s; a library product of such codes with one scale for all 94), 128 x 128 157.  Matrix cores 0.46 busy: copies alone
-// take 90 us, products and sums alone 105; codes of zeros 94 where random ones take 118, so that power decides too.  Into fp32
-// (128 x 128) 259.  Teams: 256 rows of the same 11.3 us with four on 64 x 64, 22 without; 128 x 128 18.6 with two, 26.5 without.
+// What it measured, into bf16, 8192 rows of 4096 -> 4096: 256 x 256 outputs 119 - 124 us on the same inputs again and again, 122 - 137 on three sets
+// in turn (2.3 - 2.0 PFLOP/s; a library product of such codes with one scale for all 94), 128 x 128 157 and 189.  Matrix cores 0.46 busy: copies
+// alone take 90 us, products and sums alone 105; codes of zeros 94 where random ones take 118, so that power decides too.  Into fp32
+// (128 x 128) 259 and 273 - 281: every wave converts the codes that it reads, so each is converted twice, at half of the matrix rate (floor
+// 173 - 187).  Teams, on the same inputs: 256 rows of the same 11.3 us with four on 64 x 64, 22 without; 128 x 128 18.6 with two, 26.5 without.
 __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ ((row >> 1) & 7); }
 
 // As copy16_global_to_lds_at, four bytes a lane.
@@ -703,16 +704,19 @@ bool copies_fit(const ProductArgs &a) {                          // the rows' of
   return a.x_stride < most / x_span && a.x_scales_stride < most / 4 / x_span && a.w_stride < most / 256;
 }
 
-// What a launch takes beyond an empty one, in us, for the kernels' choice; fitted to times from 1 to 8192 rows, 128 to 8192 inputs and
-// 256 to 8192 outputs (within a fifth of them where two kernels come near each other; a third with rows at odd addresses).  Such rows
-// into 16 bits have a price of their own for each step: 120 drawn calls 0.95 of the time with the factors that 32 bits keep (38 changed their kernel, 0.56 -
-// 1.36 each); for 32 bits the same did not pay (1.10 over the calls that changed).
+// What a launch takes beyond an empty one, in us, for the kernels' choice; the constants were fitted to times from 1 to 8192 rows, 128 to 8192
+// inputs and 256 to 8192 outputs.  The prices order the kernels; as times they are rough: with 2.4 us for the launch 0.84 of the
+// measured time in the median of 160 drawn calls, 0.54 - 1.13 for nine of ten, 0.3 at worst (few inputs, ragged groups).  On 140 other
+// drawn calls, each timed with every kernel that was not hopeless, the one that is taken was within 2 % of the quickest in 110,
+// 1.03 times it in the geometric mean, 1.45 at worst.
 //   direct   what its work-groups read, each its own: 9 MB/us over the whole GPU
 //   tiled    rounds of as many tiles as fit the compute units, a tile's steps over k: `one` where there is one to a compute unit, `all` where
 //            there are `slots`, and `ends` before and behind the steps.  Where the number of tiles is a guess (groups) and two fit a compute
-//            unit, a round that is begun counts by its part.
+//            unit, a round that is begun counts by its part.  (Too little for long ragged groups: 16384 rows of 2048 -> 1024 in 32 groups are priced
+//            44 with 128 x 128 and 63 with 256 x 256, and take 79 and 78; in even groups 64 and 45.)
 // What the choice is worth, us: 16 rows of 4096 -> 4096 7.2 with 16 x 16, 9.0 with 16 x 32; 256 of them 11.3 with four teams on 64 x 64, 11.6 with two, 26.5
 // with 128 x 128; 614 of 6472 -> 3900 49 with two teams on 128 x 128, 60 with one, 65 with two on 64 x 64 (into fp32 5076 of 7936 -> 711 64, 95, 83).
+// (All on the same inputs again and again.)
 inline double direct_price(double row_tiles, double rows_of_tile, int columns, const ProductArgs &a) {
   const double work_groups = row_tiles * ((a.n + columns - 1) / columns);
   return work_groups * (rows_of_tile + columns) * a.k / (9e6 * std::min(1.0, work_groups / 256));
@@ -739,7 +743,9 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows);
   const double end_block = a.k % kScaleBlock ? 2.5 : 0;          // (read, put and multiplied behind the others)
   const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
-    const double step = async || EXACT ? 1 : side == 64 ? 1.75 : 1.5;     // through registers a step waits longer
+    // Through registers a step waits longer.  Into 16 bits the step has the factor: with those of 32 bits, 12 of 120 drawn calls took other kernels, and
+    // what they take now is 0.81 of that (0.59 - 1.37 each); into 32 bits a factor for the step did not pay (1.10).
+    const double step = async || EXACT ? 1 : side == 64 ? 1.75 : 1.5;
     return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one * step, all * step, ends + end_block, std::ceil(a.k / kScaleBlock / (double)teams), GROUPED);
   };
   enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kKernels };
@@ -758,7 +764,9 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   if (!aligned)                                                  // (five dwords for every four)
     for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= EXACT ? 1.6 : 2;
   if (!async) price[kTiled256] = HUGE_VAL;                       // (its sums leave no registers to copy through)
-  if (!async && EXACT) {                                         // (through registers: steps and ends in one)
+  if (!async && EXACT) {
+    // Through registers: steps and ends in one.  The factors carry spilled registers too: a piece that is held takes five, beside fragments of
+    // bf16, and all of these but 64 x 64 with two teams spill 12 - 30 (52 - 92 bytes a lane).
     price[kTiled64x4] *= 2, price[kTiled64x2] *= 2;
     price[kTiled128x2] *= 1.5, price[kTiled128] *= 1.5;
   }

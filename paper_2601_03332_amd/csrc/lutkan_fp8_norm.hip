@@ -21,8 +21,9 @@ constexpr int kNoResidual = -1, kRowsOfGroup = 4;
 // One row is normalised by `row_waves` waves, 64 * 8 * CH columns each; a work-group holds one row, or (row_waves = 1) four.  Every
 // element is read once, stays in a register as fp32, and leaves as its sum with the residual and as its code: lane l of a row's
 // lanes holds the eight columns 8 (l + lanes c), c < CH, so that 16 neighbouring lanes hold one block of 128.
-// Bound by memory: 32768 rows of 1024 (bf16, residual bf16) 47 us, 5.0 TB/s, where a copy of 1 GiB reaches 5.1.  A few rows: the host, 5.9 us
-// a call for one row of 1024; its kernel is 2.8, one dependent chain of load, two reductions and store.
+// Bound by memory: 32768 rows of 1024 (bf16, residual bf16) 47 us, 5.0 TB/s, where a copy of 1 GiB reaches 5.1; with several waves a row
+// 8192 rows of 4096 42 - 47 us (5.6 - 5.0), 4096 of 8192 44, 2048 of 16384 46, 1024 of 32768 56 (4.3; a work-group of 16 waves has the compute unit to
+// itself).  A few rows: the host, 5.9 us a call for one row of 1024; its kernel is 2.8, one dependent chain of load, two reductions and store.
 template <int X, int R, int CH>
 __global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs a) {
   const int row_waves = a.row_waves;

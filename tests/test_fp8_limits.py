@@ -261,3 +261,25 @@ def test_every_copy_into_lds_preserves_m0_where_that_is_switched_on(tmp_path):
         else:
             block.append(text.split(";")[0].strip())
     assert min(copies.values()) > 0
+
+
+def test_registers_spill_only_in_the_kernels_that_are_priced_for_it(tmp_path):
+    """The tiled kernels into 32 bits that copy through registers hold more than fits, but for 64 x 64 with two teams; no other kernel of the
+    products has scratch memory."""
+    import os
+    import re
+    import subprocess
+    from paper_2601_03332_amd import build as lib_build
+    out = tmp_path / "matmul.s"
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")] + lib_build.HIPCC_FLAGS +
+                   ["-I", os.path.join(lib_build.ROOT, "include"), "-I", lib_build.CSRC, "-x", "hip", "--cuda-device-only", "-S", os.path.join(lib_build.CSRC, "lutkan_fp8_matmul.hip"), "-o", str(out)],
+                   check=True, capture_output=True)
+    scratch = dict(re.findall(r"\.name: +(_Z\S*lutkan_fp8_\S+)\n(?:.*\n)*?.*\.private_segment_fixed_size: +(\d+)", out.read_text()))
+    assert len(scratch) >= 40
+    for kernel, size in scratch.items():
+        shape = re.search(r"tiled_kernelI(?:Li\d+E){4}Li(\d)ELb1ELb[01]ELb0E", kernel)       # (teams; 32 bits; grouped or not; through registers)
+        small = "tiled_kernelILi2ELi2E" in kernel
+        if shape and not (small and shape.group(1) == "2"):
+            assert int(size) <= 128, (kernel, size)
+        else:
+            assert int(size) == 0, (kernel, size)
