@@ -78,6 +78,8 @@ __device__ __forceinline__ void store8(unsigned char *p, const float (&v)[8]) {
 // that a block that holds one gets a NaN scale.
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+
 // A block's scale from the largest magnitude in it; NaN stays NaN (the comparison fails).
 __device__ __forceinline__ float block_scale(unsigned largest) {
   const float s = __uint_as_float(largest) / kFp8Largest;

@@ -246,7 +246,6 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs &a, int64_t row)
 // finite, a sum of zero comes out as NaN and a small one as infinite.  Rows of the tile with such a block are computed again in
 // fp64, an output to a lane, by the wave that stored them; other rows stay as they are.  (The kernels' loops have no place to look for
 // it; this costs them one multiply-add an output.)
-__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 template <int ROWS, int COLS, bool GROUPED>
 __device__ __forceinline__ void again_in_fp64(const RowTile &t, int64_t row0, int col0) {
   static_assert(kScaleBlock % COLS == 0, "columns of one block");

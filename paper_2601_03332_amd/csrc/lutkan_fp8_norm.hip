@@ -91,20 +91,31 @@ __global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs
   };
   float first_weight[8];                                         // of a lane's only columns: asked for before the sum is known
   if constexpr (CH == 1) read_weight(8 * at, first_weight);      // (with more of them it costs registers: 32768 rows of 1024 47 -> 50 us)
-  float sum = 0.0f;
+  const auto sum_of_squares = [&](float factor) {
+    float sum = 0.0f;
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(h[c][e], h[c][e], sum);
+      for (int e = 0; e < 8; ++e) sum = fmaf(h[c][e] * factor, h[c][e] * factor, sum);
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-  if (row_waves > 1) {
-    if (lane == 0) s_sum[wave] = sum;
-    __syncthreads();
-    sum = 0.0f;
-    for (int w = 0; w < row_waves; ++w) sum += s_sum[w];
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    if (row_waves > 1) {
+      if (lane == 0) s_sum[wave] = sum;
+      __syncthreads();
+      sum = 0.0f;
+      for (int w = 0; w < row_waves; ++w) sum += s_sum[w];
+    }
+    return sum;
+  };
+  const float sum = sum_of_squares(1.0f), mean = fmaf(sum, a.inverse_width, a.eps);
+  float factor = 1.0f, inverse_rms = 1.0f / sqrtf(mean);
+  // Squares beyond fp32 (|h| above 1.8e19, or a row that holds an infinity or NaN) or below what it holds well: both over again with h times a power of 2.
+  // The largest |h| squared is then 2^96, the smallest that can bring a row here 2^-24; a sum that is too small was below 2^-85, now 2^115.
+  if (!(finite(sum) && mean >= 0x1p-100f)) {
+    factor = finite(sum) ? 0x1p100f : 0x1p-80f;
+    if (row_waves > 1) __syncthreads();                          // (the row is the work-group's: all its waves are here, and have read the first sum)
+    inverse_rms = 1.0f / sqrtf(fmaf(sum_of_squares(factor), a.inverse_width, a.eps * factor * factor));
   }
-  const float inverse_rms = 1.0f / sqrtf(fmaf(sum, a.inverse_width, a.eps));
   unsigned char *codes = a.codes + row * a.codes_stride;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -115,7 +126,7 @@ __global__ __launch_bounds__(1024) void lutkan_rmsnorm_fp8_kernel(const NormArgs
     unsigned largest = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[e] = h[c][e] * inverse_rms * (CH == 1 ? first_weight[e] : weight[e]);
+      y[e] = h[c][e] * factor * inverse_rms * (CH == 1 ? first_weight[e] : weight[e]);
       if (whole || col + e < a.width) largest = max(largest, magnitude(y[e]));      // (0 * an infinite norm beyond the row's end is none of its values)
     }
 #pragma unroll

@@ -134,6 +134,42 @@ def test_the_most_groups():
     assert torch.equal(y, expected)
 
 
+# ---------------------------------------------------------------- rows whose squares are beyond the type
+@gpu
+@pytest.mark.parametrize("rows", [8, 1100, 2100])
+@pytest.mark.parametrize("width", [7, 300, 1024, 2048, 5001, 32768])
+def test_norm_of_rows_whose_squares_are_beyond_the_type(rows, width):
+    """A row of values above 1.8e19, or without eps one below 1e-19, has a norm like any other, to what sums in fp32 give: 64 * 2^-24.  The rows around
+    it, one with an infinity and one of zeros are what they are without it."""
+    print(f"case huge and tiny rows {rows} {width}", flush=True)
+    if rows * width > 12_000_000:
+        rows = 1026 if width < 20000 else 40
+    depth = 64 * 2.0 ** -24
+    gen = torch.Generator(device=DEV).manual_seed(width)
+    x = torch.randn(rows, width, generator=gen, device=DEV)
+    x = torch.where(x.abs() < 2.0 ** -6, torch.full_like(x, 0.5), x)
+    one = torch.ones(width, device=DEV)
+    for eps in (0.0, 1e-6):
+        plain = lk.lutkan_rmsnorm_fp8(x, one, eps=eps)
+        given = x.clone()
+        for row, factor in enumerate((1e19, 1e20, 1e30, 3.0e38 / float(x[3].abs().max()), 1e-18, 1e-24, 1e-36)):
+            given[row] = x[row] * factor
+        given[7, width - 1] = float("inf")
+        codes, scales, _ = lk.lutkan_rmsnorm_fp8(given, one, eps=eps)
+        h = given[:7].double()
+        y = h / torch.sqrt(h.square().mean(1, keepdim=True) + eps)
+        blocks = -(-width // 128)
+        exact = torch.nn.functional.pad(y.abs(), (0, blocks * 128 - width)).view(7, blocks, 128).amax(2) / 448
+        assert bool(((scales[:7].double() - exact).abs() <= depth * exact).all()), eps
+        got, v = codes[:7].float().double(), y / exact.repeat_interleave(128, 1)[:, :width]
+        step = torch.exp2(torch.floor(torch.log2((v.abs() * (1 + 2 * depth)).clamp(2.0 ** -6))).clamp(max=8) - 3)
+        assert bool(((got - v).abs() <= 0.5 * step + 2 * depth * v.abs()).all()), eps
+        value = codes[7].float() * scales[7].repeat_interleave(128)[:width]
+        edge = (width - 1) // 128 * 128
+        assert bool(torch.isnan(value[edge:]).all()) and bool((value[:edge] == 0).all())
+        assert torch.equal(codes[8:].view(torch.uint8), plain[0][8:].view(torch.uint8)) and torch.equal(scales[8:], plain[1][8:])
+
+
 # ---------------------------------------------------------------- large products that cancel
 @gpu
 @pytest.mark.parametrize("shape", [(5, 384, 40), (3000, 384, 2048)], ids=str)
