@@ -457,6 +457,89 @@ typedef struct {
 int lutkan_matmul_fp8(const lutkan_matmul_fp8_args *args, void *hip_stream);
 int lutkan_grouped_matmul_fp8(const lutkan_matmul_fp8_args *args, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * The same on 8-bit integers, and a mixture of experts from the router's choices to the tokens' sums.
+ *
+ * Integer codes are whole numbers -127 .. 127, a byte each (products take -128 too); a scale (fp32) belongs to each row: to a token's
+ * activations, resp. to the inputs of one output of a weight.  A code stands for code * scale, with
+ *     scale = max(largest magnitude in the row / 127, 2^-126),    code = value / scale rounded to nearest, ties to even
+ * A row with a NaN or an infinity has the scale NaN and codes of 0, and stands for NaN.  Strides as above.
+ * ---------------------------------------------------------------------------------------------- */
+#define LUTKAN_INT8_MAX_INPUTS 131071       /* inputs of a product: the sums of 2^17 products of (-128)^2 no longer fit 32 bits */
+
+/* lutkan_rmsnorm_fp8 with integer codes and one scale a row (scales [rows], scales_stride elements apart). */
+int lutkan_rmsnorm_int8(const lutkan_rmsnorm_fp8_args *args, void *hip_stream);
+
+/* Rows [matrices][n][k] of a lutkan_type (a weight's outputs, or tokens) to codes [matrices][n][k] and scales [matrices][n], both
+ * contiguous.  k is at most LUTKAN_INT8_MAX_INPUTS.  Errors: EINVAL, ESHAPE (negative strides), EUNSUPPORTED, EHIP. */
+int lutkan_quantise_int8(const void *rows, int32_t type, int64_t matrices, int32_t n, int32_t k, int64_t stride, int64_t matrix_stride,
+                         void *codes, float *scales, void *hip_stream);
+
+/* y[s][j] = x_scales[s] * weight_scales[j] * sum over k of x[s][k] * weight[j][k].  The sum is exact (32-bit integers); its value times the
+ * scales' product is rounded to fp32 (an error of at most 3 2^-24 of y), then to y_type.  Scales may be any numbers: where they or their product leave
+ * 2^-60 .. 2^60 the row's tile is scaled in fp64.  Arguments, groups and gathered rows as of lutkan_[grouped_]matmul_fp8, with
+ * x_scales [x_rows], x_scales_stride elements apart (0: one scale for all), and weight_scales [groups][n], contiguous; a row
+ * of zeros (row_index outside x, or behind the last group) is zeros whatever the scales are.
+ * Errors as there; k at most LUTKAN_INT8_MAX_INPUTS. */
+int lutkan_matmul_int8(const lutkan_matmul_fp8_args *args, void *hip_stream);
+int lutkan_grouped_matmul_int8(const lutkan_matmul_fp8_args *args, void *hip_stream);
+
+#define LUTKAN_EXPERT_MAX LUTKAN_FP8_MAX_GROUPS     /* experts that choices are sorted by; above 2048 in two passes */
+#define LUTKAN_EXPERT_MAX_CHOICES LUTKAN_FP8_MAX_GROUPED_ROWS   /* tokens * top */
+
+/* A router's choices sorted by expert.  Choice c = t * top + j of token t is expert[t][j]; choices of one expert keep their order.  A choice
+ * outside [0, experts) is dropped: it belongs to no group and has no place.
+ *   rows         [tokens * top]   the token of each sorted row (what row_index of a grouped product takes); -1 behind the last group
+ *   places       [tokens][top]    the sorted row of each choice; -1: dropped
+ *   group_sizes  [experts]
+ * workspace: device, >= lutkan_expert_sort_workspace_bytes(tokens, top, experts) (0 for the smaller calls, one launch: up to 16384 choices and 2048 experts), 4-byte
+ * aligned, free again once the call's kernels have run.
+ * Errors: EINVAL, ESHAPE (workspace, stride), EUNSUPPORTED (experts, choices), EHIP. */
+typedef struct {
+  const void *expert;                       /* device [tokens][top], whole numbers of expert_bytes (4 or 8) */
+  int32_t *rows, *places, *group_sizes;     /* device */
+  void *workspace;
+  int64_t expert_stride;                    /* elements from one token to the next */
+  int64_t tokens;
+  size_t workspace_bytes;
+  int32_t top, experts, expert_bytes;
+} lutkan_expert_sort_args;
+size_t lutkan_expert_sort_workspace_bytes(int64_t tokens, int32_t top, int32_t experts);
+int lutkan_expert_sort(const lutkan_expert_sort_args *args, void *hip_stream);
+
+/* out[t] = sum over j of weights[t][j] * y[places[t][j]], in the order of j and in fp32, rounded once to out_type.  A place outside
+ * [0, y_rows) adds nothing, whatever its weight is; a token without a place is zeros.  weights null: 1.  With top = 1 and places = the rows of lutkan_expert_sort
+ * it brings the tokens into the experts' order; the gradient of that is the same call without weights on the places.
+ * Errors: EINVAL, ESHAPE (strides, rows), EUNSUPPORTED (strides, counts), EHIP. */
+typedef struct {
+  const void *y;                            /* device [y_rows][width] of y_type */
+  const void *places;                       /* device [tokens][top], contiguous, whole numbers of places_bytes (4 or 8) */
+  const void *weights;                      /* device [tokens][top] of weights_type, contiguous; nullable */
+  void *out;                                /* device [tokens][width] of out_type */
+  int64_t y_rows, y_stride, out_stride, tokens;
+  int32_t top, width;
+  int32_t y_type, weights_type, out_type;   /* lutkan_type */
+  int32_t places_bytes;
+} lutkan_expert_combine_args;
+int lutkan_expert_combine(const lutkan_expert_combine_args *args, void *hip_stream);
+
+/* Its gradients: grad_y[places[t][j]] = weights[t][j] * grad[t] and grad_weights[t][j] = <grad[t], y[places[t][j]]>, products and sums in fp32, rounded
+ * once.  places and rows are of one lutkan_expert_sort (rows: the token of each row of y): a place counts where rows leads back to its token;
+ * rows of grad_y that no place leads to are zeros, and so is grad_weights of a choice without a place.  Several places must not be equal.
+ * Without weights, y is not read and grad_weights not written: both null.  y and grad_y have one type, weights and grad_weights too.
+ * The order of the sums depends on the sizes, not on the run: equal calls give equal bits.  Errors as lutkan_expert_combine. */
+typedef struct {
+  const void *grad;                         /* device [tokens][width] of grad_type */
+  const void *y;                            /* device [y_rows][width] of y_type; null without weights */
+  const void *rows, *places, *weights;      /* device [y_rows], [tokens][top], [tokens][top]; contiguous; weights nullable */
+  void *grad_y, *grad_weights;              /* device [y_rows][width] of y_type, [tokens][top] of weights_type */
+  int64_t y_rows, grad_stride, y_stride, grad_y_stride, tokens;
+  int32_t top, width;
+  int32_t grad_type, y_type, weights_type;  /* lutkan_type */
+  int32_t rows_bytes, places_bytes;
+} lutkan_expert_combine_backward_args;
+int lutkan_expert_combine_backward(const lutkan_expert_combine_backward_args *args, void *hip_stream);
+
 /* Measurement aid, not part of the method: launches one kernel of known work that exercises a single resource, so
  * that a caller who times it (events on hip_stream) learns the rate this machine sustains and can put the layer
  * kernels' roofline terms beside measured peaks as well as published ones.

@@ -14,4 +14,6 @@ from .binding import (  # noqa: F401
     lutkan_forward_workspace_bytes, lutkan_last_error, lutkan_last_plan, lutkan_chain_forward, lutkan_model_forward,
     lutkan_model_workspace_bytes, lutkan_probe_launch, lutkan_version, load_library, lutkan_forward_static_scratch,
     STATIC_SCRATCH_BYTES, FP8_BLOCK, lutkan_rmsnorm_fp8, lutkan_quantise_fp8, lutkan_matmul_fp8, lutkan_grouped_matmul_fp8,
+    lutkan_rmsnorm_int8, lutkan_quantise_int8, lutkan_matmul_int8, lutkan_grouped_matmul_int8, lutkan_expert_sort, lutkan_expert_combine,
+    lutkan_expert_combine_backward,
 )

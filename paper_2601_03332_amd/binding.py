@@ -80,6 +80,24 @@ class _MatmulFp8Args(C.Structure):
                [("group_sizes_bytes", C.c_int32), ("row_index_bytes", C.c_int32)]
 
 
+class _ExpertSortArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("expert", "rows", "places", "group_sizes", "workspace")] + \
+               [("expert_stride", C.c_int64), ("tokens", C.c_int64), ("workspace_bytes", C.c_size_t)] + \
+               [(n, C.c_int32) for n in ("top", "experts", "expert_bytes")]
+
+
+class _ExpertCombineArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("y", "places", "weights", "out")] + \
+               [(n, C.c_int64) for n in ("y_rows", "y_stride", "out_stride", "tokens")] + \
+               [(n, C.c_int32) for n in ("top", "width", "y_type", "weights_type", "out_type", "places_bytes")]
+
+
+class _ExpertCombineBackwardArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("grad", "y", "rows", "places", "weights", "grad_y", "grad_weights")] + \
+               [(n, C.c_int64) for n in ("y_rows", "grad_stride", "y_stride", "grad_y_stride", "tokens")] + \
+               [(n, C.c_int32) for n in ("top", "width", "grad_type", "y_type", "weights_type", "rows_bytes", "places_bytes")]
+
+
 EXPORTS = [
     "lutkan_last_error", "lutkan_last_plan", "lutkan_version", "lutkan_compile", "lutkan_artifact_free", "lutkan_artifact_info",
     "lutkan_artifact_q", "lutkan_artifact_scale", "lutkan_artifact_ymin", "lutkan_artifact_knots",
@@ -93,6 +111,8 @@ EXPORTS = [
     "lutkan_forward_or_workspace", "lutkan_model_forward_or_workspace",
     "lutkan_wide_table_bytes", "lutkan_wide_table_build",
     "lutkan_rmsnorm_fp8", "lutkan_quantise_fp8", "lutkan_matmul_fp8", "lutkan_grouped_matmul_fp8",
+    "lutkan_rmsnorm_int8", "lutkan_quantise_int8", "lutkan_matmul_int8", "lutkan_grouped_matmul_int8",
+    "lutkan_expert_sort_workspace_bytes", "lutkan_expert_sort", "lutkan_expert_combine", "lutkan_expert_combine_backward",
 ]
 
 _lib = None
@@ -155,6 +175,15 @@ def load_library():
     lib.lutkan_quantise_fp8.argtypes = [vp, i32, i64, i32, i32, i64, i64, vp, vp, vp]
     lib.lutkan_matmul_fp8.argtypes = [C.POINTER(_MatmulFp8Args), vp]
     lib.lutkan_grouped_matmul_fp8.argtypes = [C.POINTER(_MatmulFp8Args), vp]
+    lib.lutkan_rmsnorm_int8.argtypes = [C.POINTER(_RmsnormFp8Args), vp]
+    lib.lutkan_quantise_int8.argtypes = [vp, i32, i64, i32, i32, i64, i64, vp, vp, vp]
+    lib.lutkan_matmul_int8.argtypes = [C.POINTER(_MatmulFp8Args), vp]
+    lib.lutkan_grouped_matmul_int8.argtypes = [C.POINTER(_MatmulFp8Args), vp]
+    lib.lutkan_expert_sort_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.lutkan_expert_sort_workspace_bytes.restype = sz
+    lib.lutkan_expert_sort.argtypes = [C.POINTER(_ExpertSortArgs), vp]
+    lib.lutkan_expert_combine.argtypes = [C.POINTER(_ExpertCombineArgs), vp]
+    lib.lutkan_expert_combine_backward.argtypes = [C.POINTER(_ExpertCombineBackwardArgs), vp]
     _lib = lib
     return lib
 
@@ -928,3 +957,215 @@ def lutkan_grouped_matmul_fp8(x, x_scales, weight, weight_scales, group_sizes, r
     with torch.cuda.device(x.device):
         _check(load_library().lutkan_grouped_matmul_fp8(C.byref(a), _stream(x.device)))
     return y
+
+
+# ---------------------------------------------------------------- 8-bit integers (see lutkan.h)
+def lutkan_rmsnorm_int8(x, weight, residual=None, eps: float = 1e-6, residual_out=None):
+    """lutkan_rmsnorm_fp8 with integer codes and one scale a row: returns (codes, scales, residual_out), int8 [rows, width], float32 [rows], and
+    x + residual in the residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself."""
+    who, torch = "lutkan_rmsnorm_int8", _torch()
+    _check_matrix(who, "x", x, (None, None), None)
+    rows, width = x.shape
+    _check_length(who, "a width", width)
+    _check_matrix(who, "weight", weight, (width,), x.device)
+    if residual is not None:
+        _check_matrix(who, "residual", residual, (rows, width), x.device)
+        if residual_out is None:
+            residual_out = torch.empty((rows, width), dtype=residual.dtype, device=x.device)
+        else:
+            _check_matrix(who, "residual_out", residual_out, (rows, width), x.device, residual.dtype)
+            _check_rows_apart(who, "residual_out", residual_out)
+    elif residual_out is not None:
+        raise LutKanError(f"{who}: residual_out without a residual")
+    codes = torch.empty((rows, width), dtype=torch.int8, device=x.device)
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    a = _RmsnormFp8Args(x.data_ptr(), None, weight.data_ptr(), None, codes.data_ptr(), scales.data_ptr())
+    a.x_stride, a.codes_stride, a.scales_stride, a.rows, a.width = _row_stride(x), width, 1, rows, width
+    a.x_type, a.weight_type, a.eps = _type_of(x.dtype), _type_of(weight.dtype), eps
+    if residual is not None:
+        a.residual, a.residual_out, a.residual_type = residual.data_ptr(), residual_out.data_ptr(), _type_of(residual.dtype)
+        a.residual_stride, a.residual_out_stride = _row_stride(residual), _row_stride(residual_out)
+    with torch.cuda.device(x.device):
+        _check(load_library().lutkan_rmsnorm_int8(C.byref(a), _stream(x.device)))
+    return codes, scales, residual_out
+
+
+def lutkan_quantise_int8(x):
+    """(codes, scales) of a weight [n, k], of one weight per expert [experts, n, k], or of tokens [rows, k]: int8 of x's shape and a float32 scale
+    for each row of it ([n], [experts, n], [rows]), for the products below."""
+    who, torch = "lutkan_quantise_int8", _torch()
+    _check_matrix(who, "x", x, (None,) * (3 if isinstance(x, torch.Tensor) and x.dim() == 3 else 2), None)
+    n, k = x.shape[-2:]
+    _check_length(who, "rows", n)
+    _check_length(who, "inputs", k)
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    with torch.cuda.device(x.device):
+        _check(load_library().lutkan_quantise_int8(x.data_ptr(), _type_of(x.dtype), x.shape[0] if x.dim() == 3 else 1, n, k, _row_stride(x),
+                                                   x.stride(0) if x.dim() == 3 else 0, codes.data_ptr(), scales.data_ptr(), _stream(x.device)))
+    return codes, scales
+
+
+def _matmul_int8(who, x, x_scales, weight, weight_scales, y, dtype, rows, experts):
+    """The checks and arguments that the two products share; `rows` of y, None: as many as x."""
+    torch = _torch()
+    _check_matrix(who, "x", x, (None, None), None, torch.int8)
+    k, device = x.shape[1], x.device
+    _check_matrix(who, "weight", weight, (None, None, k) if experts else (None, k), device, torch.int8)
+    n = weight.shape[-2]
+    for what, length in (("inputs", k), ("outputs", n), ("weights", weight.shape[0] if experts else 1)):
+        _check_length(who, what, length)
+    for t, what, shape in ((x_scales, "x_scales", x.shape[:1]), (weight_scales, "weight_scales", weight.shape[:-1])):
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != torch.float32 or t.layout != torch.strided or t.device != device:
+            raise LutKanError(f"{who}: {what} must be a float32 tensor of shape {list(shape)} on {device}")
+    if not weight_scales.is_contiguous():
+        raise LutKanError(f"{who}: weight_scales must be contiguous")
+    rows = x.shape[0] if rows is None else rows
+    if y is None:
+        if _type_of(dtype) is None:
+            raise LutKanError(f"{who}: dtype must be float32, float16 or bfloat16")
+        y = torch.empty((rows, n), dtype=dtype, device=device)
+    else:
+        _check_matrix(who, "y", y, (rows, n), device)
+        _check_rows_apart(who, "y", y)
+    return y, _MatmulFp8Args(x.data_ptr(), x_scales.data_ptr(), weight.data_ptr(), weight_scales.data_ptr(), y.data_ptr(), x.shape[0], _row_stride(x),
+                             x_scales.stride(0), _row_stride(weight), weight.stride(0) if experts else 0, _row_stride(y), rows, k, n, _type_of(y.dtype))
+
+
+def lutkan_matmul_int8(x, x_scales, weight, weight_scales, y=None, dtype=None):
+    """y [rows, n] = x [rows, k] times weight [n, k] transposed, both as codes (int8) with a scale for each row, x_scales [rows] and weight_scales [n]
+    (of lutkan_rmsnorm_int8 and lutkan_quantise_int8, or a checkpoint's), on the current stream.  The sums are exact.  dtype: of y where none
+    is given (float32, which a layer takes, is the default; float16, bfloat16)."""
+    who, torch = "lutkan_matmul_int8", _torch()
+    dtype = torch.float32 if dtype is None else dtype
+    y, a = _matmul_int8(who, x, x_scales, weight, weight_scales, y, dtype, None, False)
+    with torch.cuda.device(x.device):
+        _check(load_library().lutkan_matmul_int8(C.byref(a), _stream(x.device)))
+    return y
+
+
+def _check_whole_numbers(who, what, t, device=None, shape=None):
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or not t.is_cuda or t.layout != torch.strided or not t.is_contiguous():
+        raise LutKanError(f"{who}: {what} must be a contiguous int32 or int64 CUDA tensor")
+    if shape is not None and t.shape != shape:
+        raise LutKanError(f"{who}: {what} must be of shape {list(shape)}")
+    if device is not None and t.device != device:
+        raise LutKanError(f"{who}: {what} is on {t.device}, the others are on {device}")
+
+
+def lutkan_grouped_matmul_int8(x, x_scales, weight, weight_scales, group_sizes, rows=None, y=None, dtype=None):
+    """lutkan_matmul_int8 by expert: weight [experts, n, k], weight_scales [experts, n], the rows of y in groups, one after the other, group e the
+    next group_sizes[e] rows (int32 or int64 [experts], on the device; nothing waits for it); rows of y behind the last group are zeros.
+    rows: int32 or int64 [rows of y], which row of x each row of y comes from (outside x: a row of zeros); None: its own.  Both as
+    lutkan_expert_sort gives them."""
+    who, torch = "lutkan_grouped_matmul_int8", _torch()
+    dtype = torch.float32 if dtype is None else dtype
+    _check_matrix(who, "x", x, (None, None), None, torch.int8)
+    if rows is not None:
+        _check_whole_numbers(who, "rows", rows, x.device)
+        if rows.dim() != 1:
+            raise LutKanError(f"{who}: rows must have one dimension")
+    y, a = _matmul_int8(who, x, x_scales, weight, weight_scales, y, dtype, None if rows is None else rows.numel(), True)
+    _check_whole_numbers(who, "group_sizes", group_sizes, x.device, weight.shape[:1])
+    a.groups, a.group_sizes, a.group_sizes_bytes = weight.shape[0], group_sizes.data_ptr(), group_sizes.element_size()
+    if rows is not None:
+        a.row_index, a.row_index_bytes = rows.data_ptr(), rows.element_size()
+    with torch.cuda.device(x.device):
+        _check(load_library().lutkan_grouped_matmul_int8(C.byref(a), _stream(x.device)))
+    return y
+
+
+# ---------------------------------------------------------------- a mixture of experts: choices sorted, rows joined (see lutkan.h)
+def lutkan_expert_sort(expert, experts: int):
+    """A router's choices expert [tokens, top] (int32 or int64) sorted by expert, those of one expert in their order, on the current stream; nothing
+    waits for it.  Returns int32 tensors (rows, places, group_sizes):
+        rows [tokens * top]   the token of each sorted row, -1 behind the last group (rows= of the grouped products)
+        places [tokens, top]  the sorted row of each choice; -1 for a choice outside [0, experts), which belongs to no group
+        group_sizes [experts]"""
+    who, torch = "lutkan_expert_sort", _torch()
+    if not isinstance(expert, torch.Tensor) or expert.dtype not in (torch.int32, torch.int64) or expert.dim() != 2 or not expert.is_cuda or expert.layout != torch.strided:
+        raise LutKanError(f"{who}: expert must be an int32 or int64 CUDA tensor of shape [tokens, top]")
+    tokens, top = expert.shape
+    if top > 1 and expert.stride(1) != 1:
+        raise LutKanError(f"{who}: expert must have contiguous columns")
+    experts = int(experts)
+    _check_length(who, "choices a token", top)
+    _check_length(who, "experts", experts)
+    lib = load_library()
+    rows = torch.empty(tokens * top, dtype=torch.int32, device=expert.device)
+    places = torch.empty((tokens, top), dtype=torch.int32, device=expert.device)
+    group_sizes = torch.empty(max(experts, 0), dtype=torch.int32, device=expert.device)
+    need = lib.lutkan_expert_sort_workspace_bytes(tokens, top, experts)
+    workspace = torch.empty(need, dtype=torch.uint8, device=expert.device)
+    a = _ExpertSortArgs(expert.data_ptr(), rows.data_ptr(), places.data_ptr(), group_sizes.data_ptr(), workspace.data_ptr(),
+                        expert.stride(0) if tokens > 1 else top, tokens, need, top, experts, expert.element_size())
+    with torch.cuda.device(expert.device):
+        _check(lib.lutkan_expert_sort(C.byref(a), _stream(expert.device)))
+    return rows, places, group_sizes
+
+
+def _check_weights(who, weights, shape, device):
+    if weights is not None:
+        _check_matrix(who, "weights", weights, shape, device)
+        if not weights.is_contiguous():
+            raise LutKanError(f"{who}: weights must be contiguous")
+
+
+def lutkan_expert_combine(y, places, weights=None, out=None, dtype=None):
+    """out [tokens, width] = for each token the sum over its places of weight * y[place], y [rows, width], places [tokens, top] (int32 or int64, as
+    lutkan_expert_sort gives them), weights [tokens, top] or None (1), on the current stream; summed in float32.  A place outside y adds nothing.
+    dtype: of out where none is given (y's).  lutkan_expert_combine(x, rows[:, None]) brings tokens x into the experts' order, a row of zeros
+    where rows is -1; the gradient of that is lutkan_expert_combine(gradient, places)."""
+    who, torch = "lutkan_expert_combine", _torch()
+    _check_matrix(who, "y", y, (None, None), None)
+    _check_whole_numbers(who, "places", places, y.device)
+    if places.dim() != 2:
+        raise LutKanError(f"{who}: places must be of shape [tokens, top]")
+    _check_weights(who, weights, places.shape, y.device)
+    tokens, top = places.shape
+    width = y.shape[1]
+    _check_length(who, "a width", width)
+    _check_length(who, "choices a token", top)
+    if out is None:
+        dtype = y.dtype if dtype is None else dtype
+        if _type_of(dtype) is None:
+            raise LutKanError(f"{who}: dtype must be float32, float16 or bfloat16")
+        out = torch.empty((tokens, width), dtype=dtype, device=y.device)
+    else:
+        _check_matrix(who, "out", out, (tokens, width), y.device)
+        _check_rows_apart(who, "out", out)
+    a = _ExpertCombineArgs(y.data_ptr(), places.data_ptr(), None if weights is None else weights.data_ptr(), out.data_ptr(), y.shape[0], _row_stride(y),
+                           _row_stride(out), tokens, top, width, _type_of(y.dtype), 0 if weights is None else _type_of(weights.dtype), _type_of(out.dtype),
+                           places.element_size())
+    with torch.cuda.device(y.device):
+        _check(load_library().lutkan_expert_combine(C.byref(a), _stream(y.device)))
+    return out
+
+
+def lutkan_expert_combine_backward(grad, y, rows, places, weights=None):
+    """The gradients of lutkan_expert_combine(y, places, weights) for the gradient grad [tokens, width] of its output: (grad_y [rows, width] in y's
+    dtype, grad_weights [tokens, top] in the weights'; None without weights).  rows and places are of one lutkan_expert_sort; rows of grad_y that
+    no place leads to are zeros.  The operators take no part in torch's autograd: a program calls this from its own backward pass."""
+    who, torch = "lutkan_expert_combine_backward", _torch()
+    _check_matrix(who, "grad", grad, (None, None), None)
+    tokens, width = grad.shape
+    _check_length(who, "a width", width)
+    _check_matrix(who, "y", y, (None, width), grad.device)
+    _check_whole_numbers(who, "rows", rows, grad.device, y.shape[:1])
+    _check_whole_numbers(who, "places", places, grad.device)
+    if places.dim() != 2 or places.shape[0] != tokens:
+        raise LutKanError(f"{who}: places must be of shape [{tokens}, top]")
+    _check_weights(who, weights, places.shape, grad.device)
+    top = places.shape[1]
+    _check_length(who, "choices a token", top)
+    grad_y = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+    grad_weights = None if weights is None else torch.empty(weights.shape, dtype=weights.dtype, device=y.device)
+    a = _ExpertCombineBackwardArgs(grad.data_ptr(), None if weights is None else y.data_ptr(), rows.data_ptr(), places.data_ptr(), None, grad_y.data_ptr(), None,
+                                   y.shape[0], _row_stride(grad), _row_stride(y), width, tokens, top, width, _type_of(grad.dtype), _type_of(y.dtype), 0,
+                                   rows.element_size(), places.element_size())
+    if weights is not None:
+        a.weights, a.grad_weights, a.weights_type = weights.data_ptr(), grad_weights.data_ptr(), _type_of(weights.dtype)
+    with torch.cuda.device(grad.device):
+        _check(load_library().lutkan_expert_combine_backward(C.byref(a), _stream(grad.device)))
+    return grad_y, grad_weights

@@ -1,0 +1,437 @@
+// A mixture of experts around the products by expert: a router's choices sorted by expert, and the experts' rows back in the tokens' order,
+// weighted, with the gradients.
+#include "lutkan_fp8.h"
+
+namespace {
+
+__device__ __forceinline__ int64_t whole_number(const void *p, int64_t at, int bytes) {
+  return bytes == 8 ? static_cast<const int64_t *>(p)[at] : static_cast<const int32_t *>(p)[at];
+}
+
+// ---- sort ----------------------------------------------------------------------------------------------------------
+// Choices are sorted by expert in one pass of a counting sort where there are few experts, and by the low, then the high bits of the expert where there
+// are more than its counters hold.
+struct SortArgs {
+  const void *expert;
+  int32_t *rows, *places, *group_sizes;                           // nullable: of another pass, resp. counted from the sorted experts
+  const int32_t *order;                                           // the choices as the pass before left them; nullable: as they are
+  int32_t *order_out, *sorted;                                    // the pass's order, the sorted choices' experts; nullable
+  int32_t *counts;                                                // [work-group][bins], several work-groups
+  int64_t stride;
+  int32_t choices, top, experts, bins;
+  int32_t segment;                                                // choices of a wave, a multiple of 64
+  int8_t expert_bytes, shift;                                     // a bin: the bits of the expert from here on
+};
+static_assert(sizeof(SortArgs) <= 112, "launch");
+
+constexpr int kSortWaves = 16;
+constexpr int kSortSingle = 16384;                                // choices of one work-group's launch
+constexpr int kSortDigit = 11, kSortBins = (1 << kSortDigit) + 1; // (2048 experts and the dropped ones)
+
+// The expert of choice c, `experts` for a choice that is dropped.
+__device__ __forceinline__ int expert_of(const SortArgs &a, int c) {
+  const int token = c / a.top;
+  const int64_t e = whole_number(a.expert, token * a.stride + (c - token * a.top), a.expert_bytes);
+  return e >= 0 && e < a.experts ? (int)e : a.experts;
+}
+// (One pass: all bits.)
+__device__ __forceinline__ int bin_of(const SortArgs &a, int expert) { return a.bins == 1 << kSortDigit ? (expert >> a.shift) & (a.bins - 1) : expert; }
+
+// Lanes with the same bin as the own one, among those that hold a choice.
+__device__ __forceinline__ unsigned long long same_bin(int bin, int bits, bool held) {
+  unsigned long long same = __ballot(held);
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long set = __ballot((bin >> b) & 1);
+    same &= (bin >> b) & 1 ? set : ~set;
+  }
+  return same;
+}
+
+// How many choices of each bin the work-group's waves hold: s_count [wave][bins].
+__device__ __forceinline__ void count_bins(const SortArgs &a, int *s_count, int first, int last, int wave, int waves) {
+  for (int i = threadIdx.x; i < waves * a.bins; i += blockDim.x) s_count[i] = 0;
+  __syncthreads();
+  for (int i = first + (threadIdx.x & 63); i < last; i += 64) atomicAdd(&s_count[wave * a.bins + bin_of(a, expert_of(a, a.order ? a.order[i] : i))], 1);
+  __syncthreads();
+}
+
+__global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_count_kernel(const SortArgs a) {
+  extern __shared__ int s_count[];
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int64_t first = ((int64_t)blockIdx.x * waves + wave) * a.segment;
+  count_bins(a, s_count, (int)min(first, (int64_t)a.choices), (int)min(first + a.segment, (int64_t)a.choices), wave, waves);
+  for (int e = threadIdx.x; e < a.bins; e += blockDim.x) {
+    int sum = 0;
+    for (int w = 0; w < waves; ++w) sum += s_count[w * a.bins + e];
+    a.counts[(int64_t)blockIdx.x * a.bins + e] = sum;
+  }
+}
+
+// A counting sort: the place of a choice is the number of choices of lower bins, of its bin in work-groups and waves before its own, and before it
+// in its wave.  The last comes from ballots over the bits of the bin, so that equal bins keep their order and no atomic decides it.
+template <bool SEVERAL>
+__global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_sort_kernel(const SortArgs a) {
+  extern __shared__ int s_count[];                                // [waves][bins], then the bins' first places and totals, then the waves' sums
+  const int bins = a.bins, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  int *s_total = s_count + waves * bins, *s_wave = s_total + bins;
+  const int64_t begin = ((int64_t)blockIdx.x * waves + wave) * a.segment;
+  const int first = (int)min(begin, (int64_t)a.choices), last = (int)min(begin + a.segment, (int64_t)a.choices);
+  count_bins(a, s_count, first, last, wave, waves);
+  // Every bin: its total and, in place of the waves' counts, how many of it lie before each wave.
+  for (int e = threadIdx.x; e < bins; e += blockDim.x) {
+    int before = 0, total = 0;
+    if constexpr (SEVERAL) {
+      for (unsigned g = 0; g < gridDim.x; ++g) {
+        const int n = a.counts[(int64_t)g * bins + e];
+        before += g < blockIdx.x ? n : 0;
+        total += n;
+      }
+    }
+    for (int w = 0; w < waves; ++w) {
+      const int n = s_count[w * bins + e];
+      s_count[w * bins + e] = before;
+      before += n;
+    }
+    s_total[e] = SEVERAL ? total : before;
+  }
+  __syncthreads();
+  // The bins' first places: sums of runs of bins, a run to a thread, then the run itself.
+  const int run = (bins + blockDim.x - 1) / blockDim.x, run_first = min((int)threadIdx.x * run, bins), run_last = min(run_first + run, bins);
+  int sum = 0;
+  for (int e = run_first; e < run_last; ++e) sum += s_total[e];
+  int with = sum;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int v = __shfl_up(with, off);
+    with += lane >= off ? v : 0;
+  }
+  if (lane == 63) s_wave[wave] = with;
+  __syncthreads();
+  int at = with - sum;
+  for (int w = 0; w < wave; ++w) at += s_wave[w];
+  for (int e = run_first; e < run_last; ++e) {
+    const int n = s_total[e];
+    if (a.group_sizes && blockIdx.x == 0 && e < a.experts) a.group_sizes[e] = n;
+    s_total[e] = at;
+    at += n;
+  }
+  __syncthreads();
+  const int bits = 32 - __builtin_clz(bins - 1);                  // (bins >= 2)
+  for (int i0 = first; i0 < last; i0 += 64) {
+    const int i = i0 + lane;
+    const bool here = i < last;
+    const int c = !here ? 0 : a.order ? a.order[i] : i, expert = here ? expert_of(a, c) : 0, bin = bin_of(a, expert);
+    const unsigned long long same = same_bin(bin, bits, here);
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    if (here) {
+      const int place = s_total[bin] + s_count[wave * bins + bin] + rank;
+      const bool held = expert < a.experts;
+      if (a.rows) {
+        a.rows[place] = held ? c / a.top : -1;
+        a.places[c] = held ? place : -1;
+      }
+      if (a.order_out) a.order_out[place] = c;
+      if (a.sorted) a.sorted[place] = expert;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // all lanes have read the count before its first lane raises it
+    if (here && rank == 0) s_count[wave * bins + bin] += __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// How many of the sorted experts are below e.
+__device__ __forceinline__ int below(const int32_t *sorted, int n, int e) {
+  int low = 0, high = n;
+  while (low < high) {
+    const int mid = low + (high - low) / 2;
+    if (sorted[mid] < e) low = mid + 1;
+    else high = mid;
+  }
+  return low;
+}
+__global__ __launch_bounds__(256) void lutkan_expert_sizes_kernel(const int32_t *sorted, int32_t choices, int32_t experts, int32_t *group_sizes) {
+  const int e = blockIdx.x * 256 + threadIdx.x;
+  if (e < experts) group_sizes[e] = below(sorted, choices, e + 1) - below(sorted, choices, e);
+}
+
+// Waves of a work-group and choices of a wave: one work-group up to kSortSingle choices, else at most 256.
+struct SortPlan {
+  int waves, segment, groups, bins;
+  bool one_pass;
+  size_t count_words, words;                                      // of the workspace: counts, then the two orders
+};
+SortPlan plan_sort(int64_t choices, int experts) {
+  SortPlan p;
+  const int64_t chunks = (choices + 63) / 64;
+  if (choices <= kSortSingle) {
+    p.waves = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, kSortWaves));
+    p.segment = (int)((chunks + p.waves - 1) / p.waves * 64);
+    p.groups = 1;
+  } else {
+    const int64_t of_wave = std::max<int64_t>(4, (chunks + 256 * kSortWaves - 1) / (256 * kSortWaves));
+    p.waves = kSortWaves;
+    p.segment = (int)(of_wave * 64);
+    p.groups = (int)((chunks + of_wave * kSortWaves - 1) / (of_wave * kSortWaves));
+  }
+  p.one_pass = experts < kSortBins;
+  p.bins = p.one_pass ? experts + 1 : 1 << kSortDigit;
+  p.count_words = p.groups > 1 ? (size_t)p.groups * p.bins : 0;
+  p.words = p.count_words + (p.one_pass ? 0 : 2 * (size_t)choices);
+  return p;
+}
+
+int launch_sort(const SortArgs &a, const SortPlan &p, const char *who, hipStream_t s) {
+  static LdsCap caps[3];
+  const size_t counts = (size_t)p.waves * p.bins * sizeof(int), lds = counts + ((size_t)p.bins + kSortWaves) * sizeof(int);
+  lutkan::plan_note("expert_sort groups=%d waves=%d; ", p.groups, p.waves);
+  if (p.groups == 1) {
+    if (int rc = raise_lds_cap(lutkan_expert_sort_kernel<false>, &caps[0], who)) return rc;
+    hipLaunchKernelGGL(lutkan_expert_sort_kernel<false>, dim3(1), dim3(64 * p.waves), lds, s, a);
+    return check_launch(who);
+  }
+  if (int rc = raise_lds_cap(lutkan_expert_count_kernel, &caps[1], who)) return rc;
+  if (int rc = raise_lds_cap(lutkan_expert_sort_kernel<true>, &caps[2], who)) return rc;
+  hipLaunchKernelGGL(lutkan_expert_count_kernel, dim3(p.groups), dim3(64 * p.waves), counts, s, a);
+  if (int rc = check_launch(who)) return rc;
+  hipLaunchKernelGGL(lutkan_expert_sort_kernel<true>, dim3(p.groups), dim3(64 * p.waves), lds, s, a);
+  return check_launch(who);
+}
+
+// ---- combine -------------------------------------------------------------------------------------------------------
+struct CombineArgs {
+  const unsigned char *y, *weights;
+  const void *places;
+  unsigned char *out;
+  int64_t y_stride, out_stride, y_rows, tokens;
+  int32_t top, width, weights_type, places_bytes;
+};
+static_assert(sizeof(CombineArgs) <= 112, "launch");
+
+__device__ __forceinline__ float weight_at(const unsigned char *weights, int type, int64_t at) {
+  const unsigned char *p = weights + at * type_bytes(type);
+  return type == LUTKAN_F32 ? load_one<LUTKAN_F32>(p) : type == LUTKAN_F16 ? load_one<LUTKAN_F16>(p) : load_one<LUTKAN_BF16>(p);
+}
+__device__ __forceinline__ void store_weight(unsigned char *weights, int type, int64_t at, float v) {
+  unsigned char *p = weights + at * type_bytes(type);
+  if (type == LUTKAN_F32) store_one<LUTKAN_F32>(p, v);
+  else if (type == LUTKAN_F16) store_one<LUTKAN_F16>(p, v);
+  else store_one<LUTKAN_BF16>(p, v);
+}
+
+// Eight columns of a row from col on, zeros behind its end.
+template <int TYPE>
+__device__ __forceinline__ void read8(const unsigned char *row, int col, int width, float (&v)[8]) {
+  if (col + 8 <= width) { values8<TYPE>(load_raw8<TYPE>(row + (size_t)col * type_bytes(TYPE)), v); return; }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = col + e < width ? load_one<TYPE>(row + (size_t)(col + e) * type_bytes(TYPE)) : 0.0f;
+}
+template <int TYPE>
+__device__ __forceinline__ void write8(unsigned char *row, int col, int width, const float (&v)[8]) {
+  if (col + 8 <= width) { store8<TYPE>(row + (size_t)col * type_bytes(TYPE), v); return; }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) if (col + e < width) store_one<TYPE>(row + (size_t)(col + e) * type_bytes(TYPE), v[e]);
+}
+
+// A wave sums 512 columns of one token, eight a lane.
+template <int Y, int O>
+__global__ __launch_bounds__(256) void lutkan_expert_combine_kernel(const CombineArgs a) {
+  const int lane = threadIdx.x & 63, pieces = (a.width + 511) / 512;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), token = unit / pieces;
+  if (token >= a.tokens) return;
+  const int col = (int)(unit - token * pieces) * 512 + 8 * lane;
+  float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  for (int j = 0; j < a.top; ++j) {
+    const int64_t place = whole_number(a.places, token * a.top + j, a.places_bytes);
+    if (place < 0 || place >= a.y_rows || col >= a.width) continue;
+    float v[8];
+    read8<Y>(a.y + place * a.y_stride * type_bytes(Y), col, a.width, v);
+    const float w = a.weights ? weight_at(a.weights, a.weights_type, token * a.top + j) : 1.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += w * v[e];             // (two roundings, as an elementwise product and a sum have)
+  }
+  if (col < a.width) write8<O>(a.out + token * a.out_stride * type_bytes(O), col, a.width, sum);
+}
+
+struct BackwardArgs {
+  const unsigned char *grad, *y, *weights;
+  const void *rows, *places;
+  unsigned char *grad_y, *grad_weights;
+  int64_t y_rows, tokens;
+  int32_t grad_stride, y_stride, grad_y_stride;
+  int32_t top, width;
+  int8_t weights_type, rows_bytes, places_bytes;
+};
+static_assert(sizeof(BackwardArgs) <= 112, "launch");
+
+// A work-group takes a token: its waves share the columns, and their sums meet in LDS in the waves' order.  Work-groups behind the last token's look through the rows of y
+// for those that no place leads to, 64 each.
+template <int G, int Y>
+__global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(const BackwardArgs a) {
+  __shared__ float s_sum[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  if (blockIdx.x >= a.tokens) {
+    const int64_t row = ((int64_t)blockIdx.x - a.tokens) * 64 + lane;
+    bool found = row >= a.y_rows;
+    if (!found) {
+      const int64_t token = whole_number(a.rows, row, a.rows_bytes);
+      if (token >= 0 && token < a.tokens)
+        for (int j = 0; j < a.top && !found; ++j) found = whole_number(a.places, token * a.top + j, a.places_bytes) == row;
+    }
+    const float zeros[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    for (unsigned long long left = __ballot(!found); left != 0; left &= left - 1) {
+      unsigned char *to = a.grad_y + (row - lane + __builtin_ctzll(left)) * a.grad_y_stride * type_bytes(Y);
+      for (int col = 8 * (int)threadIdx.x; col < a.width; col += 8 * blockDim.x) write8<Y>(to, col, a.width, zeros);
+    }
+    return;
+  }
+  const int64_t token = blockIdx.x;
+  const unsigned char *grad = a.grad + token * a.grad_stride * type_bytes(G);
+  for (int j = 0; j < a.top; ++j) {
+    const int64_t place = whole_number(a.places, token * a.top + j, a.places_bytes);
+    const bool held = place >= 0 && place < a.y_rows && whole_number(a.rows, place, a.rows_bytes) == token;      // (the work-group's: token, j)
+    const float w = held && a.weights ? weight_at(a.weights, a.weights_type, token * a.top + j) : 1.0f;
+    float dot = 0.0f;
+    for (int col = 8 * (int)threadIdx.x; held && col < a.width; col += 8 * blockDim.x) {
+      float g[8], v[8];
+      read8<G>(grad, col, a.width, g);
+      if (a.weights) {
+        read8<Y>(a.y + place * a.y_stride * type_bytes(Y), col, a.width, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = fmaf(g[e], v[e], dot);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] *= w;
+      write8<Y>(a.grad_y + place * a.grad_y_stride * type_bytes(Y), col, a.width, g);
+    }
+    if (!a.weights) continue;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off);
+    if (waves > 1) {
+      if (lane == 0) s_sum[wave] = dot;
+      __syncthreads();
+      dot = 0.0f;
+      for (int o = 0; o < waves; ++o) dot += s_sum[o];
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) store_weight(a.grad_weights, a.weights_type, token * a.top + j, held ? dot : 0.0f);
+  }
+}
+
+template <typename F>
+void with_types(int first, int second, const F &f) {
+  const auto inner = [&](auto one) {
+    switch (second) {
+      case LUTKAN_F32: f(one, std::integral_constant<int, LUTKAN_F32>()); break;
+      case LUTKAN_F16: f(one, std::integral_constant<int, LUTKAN_F16>()); break;
+      default: f(one, std::integral_constant<int, LUTKAN_BF16>()); break;
+    }
+  };
+  switch (first) {
+    case LUTKAN_F32: inner(std::integral_constant<int, LUTKAN_F32>()); break;
+    case LUTKAN_F16: inner(std::integral_constant<int, LUTKAN_F16>()); break;
+    default: inner(std::integral_constant<int, LUTKAN_BF16>()); break;
+  }
+}
+
+constexpr int kMostWidth = 1 << 30;                               // (columns are counted in 32 bits, past a row's end too)
+
+bool is_whole(int bytes) { return bytes == 4 || bytes == 8; }
+
+// What both directions check: the counts and the tokens' rows.
+int check_tokens(const char *who, int64_t tokens, int32_t top, int32_t width, int64_t y_rows) {
+  if (tokens < 0 || top < 1 || width < 1 || y_rows < 0) return fail(LUTKAN_EINVAL, "%s: %lld tokens, %d each, width %d, %lld rows", who, (long long)tokens, top, width, (long long)y_rows);
+  if (width > kMostWidth) return fail(LUTKAN_EUNSUPPORTED, "%s: width %d, at most %d", who, width, kMostWidth);
+  if (tokens > INT32_MAX || y_rows > INT32_MAX) return fail(LUTKAN_EUNSUPPORTED, "%s: at most 2^31 - 1 tokens and rows", who);
+  return LUTKAN_OK;
+}
+
+}  // namespace
+
+extern "C" size_t lutkan_expert_sort_workspace_bytes(int64_t tokens, int32_t top, int32_t experts) {
+  if (tokens < 0 || top < 1 || experts < 1 || experts > LUTKAN_EXPERT_MAX || tokens > LUTKAN_EXPERT_MAX_CHOICES / top) return 0;
+  return plan_sort(tokens * top, experts).words * sizeof(int32_t);
+}
+
+extern "C" int lutkan_expert_sort(const lutkan_expert_sort_args *p, void *hip_stream) {
+  const char *who = "lutkan_expert_sort";
+  if (!p) return fail(LUTKAN_EINVAL, "%s: null arguments", who);
+  if (p->tokens < 0 || p->top < 1 || p->experts < 1) return fail(LUTKAN_EINVAL, "%s: %lld tokens, %d each of %d experts", who, (long long)p->tokens, p->top, p->experts);
+  if (p->experts > LUTKAN_EXPERT_MAX) return fail(LUTKAN_EUNSUPPORTED, "%s: %d experts, at most %d", who, p->experts, LUTKAN_EXPERT_MAX);
+  if (p->tokens > LUTKAN_EXPERT_MAX_CHOICES / p->top) return fail(LUTKAN_EUNSUPPORTED, "%s: %lld tokens, %d each, at most %d in all", who, (long long)p->tokens, p->top, LUTKAN_EXPERT_MAX_CHOICES);
+  if (!is_whole(p->expert_bytes)) return fail(LUTKAN_EINVAL, "%s: expert is whole numbers of 4 or 8 bytes", who);
+  if (!p->group_sizes || (p->tokens > 0 && (!p->expert || !p->rows || !p->places))) return fail(LUTKAN_EINVAL, "%s: null expert / rows / places / group_sizes", who);
+  if (p->expert_stride < 0 || p->expert_stride > INT64_MAX / 8 / std::max<int64_t>(p->tokens, 1)) return fail(LUTKAN_ESHAPE, "%s: stride", who);
+  const size_t needed = lutkan_expert_sort_workspace_bytes(p->tokens, p->top, p->experts);
+  if (p->workspace_bytes < needed || (needed && !p->workspace)) return fail(LUTKAN_ESHAPE, "%s: workspace of %zu bytes, needs %zu", who, p->workspace_bytes, needed);
+  if (needed && (reinterpret_cast<uintptr_t>(p->workspace) & 3)) return fail(LUTKAN_EINVAL, "%s: workspace must be 4-byte aligned", who);
+  const SortPlan plan = plan_sort(p->tokens * p->top, p->experts);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  SortArgs a{};
+  a.expert = p->expert; a.rows = p->rows; a.places = p->places; a.group_sizes = p->group_sizes; a.counts = static_cast<int32_t *>(p->workspace);
+  a.stride = p->expert_stride; a.choices = (int32_t)(p->tokens * p->top); a.top = p->top; a.experts = p->experts; a.expert_bytes = (int8_t)p->expert_bytes;
+  a.bins = plan.bins; a.segment = plan.segment;
+  lutkan::plan_clear();
+  if (plan.one_pass) return launch_sort(a, plan, who, s);
+  int32_t *order = a.counts + plan.count_words, *sorted = order + a.choices;
+  a.rows = a.places = a.group_sizes = nullptr;
+  a.order_out = order;
+  if (int rc = launch_sort(a, plan, who, s)) return rc;
+  a.rows = p->rows; a.places = p->places;
+  a.order = order; a.order_out = nullptr; a.sorted = sorted; a.shift = kSortDigit;
+  if (int rc = launch_sort(a, plan, who, s)) return rc;
+  hipLaunchKernelGGL(lutkan_expert_sizes_kernel, dim3((p->experts + 255) / 256), dim3(256), 0, s, sorted, a.choices, p->experts, p->group_sizes);
+  return check_launch(who);
+}
+
+extern "C" int lutkan_expert_combine(const lutkan_expert_combine_args *p, void *hip_stream) {
+  const char *who = "lutkan_expert_combine";
+  if (!p) return fail(LUTKAN_EINVAL, "%s: null arguments", who);
+  if (int rc = check_tokens(who, p->tokens, p->top, p->width, p->y_rows)) return rc;
+  if (!is_type(p->y_type) || !is_type(p->out_type) || (p->weights && !is_type(p->weights_type))) return fail(LUTKAN_EINVAL, "%s: bad type", who);
+  if (!is_whole(p->places_bytes)) return fail(LUTKAN_EINVAL, "%s: places are whole numbers of 4 or 8 bytes", who);
+  if (p->tokens == 0) return LUTKAN_OK;
+  if ((p->y_rows > 0 && !p->y) || !p->places || !p->out) return fail(LUTKAN_EINVAL, "%s: null y / places / out", who);
+  if (p->y_stride < 0 || p->out_stride < p->width) return fail(LUTKAN_ESHAPE, "%s: a negative stride, or a row of out that is longer than its stride", who);
+  if (p->y_stride > INT32_MAX || p->out_stride > INT32_MAX) return fail(LUTKAN_EUNSUPPORTED, "%s: row strides of at most 2^31 - 1", who);
+  CombineArgs a;
+  a.y = static_cast<const unsigned char *>(p->y); a.weights = static_cast<const unsigned char *>(p->weights);
+  a.y_stride = p->y_stride; a.out_stride = p->out_stride; a.y_rows = p->y_rows;
+  a.top = p->top; a.width = p->width; a.weights_type = p->weights_type; a.places_bytes = p->places_bytes;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const int64_t pieces = ((int64_t)p->width + 511) / 512, launch_tokens = lutkan::kMaxLaunchThreads / 256 * 4 / pieces;      // (more tokens: more launches)
+  for (int64_t first = 0; first < p->tokens; first += launch_tokens) {
+    a.tokens = std::min(p->tokens - first, launch_tokens);
+    a.places = static_cast<const unsigned char *>(p->places) + first * p->top * p->places_bytes;
+    if (p->weights) a.weights = static_cast<const unsigned char *>(p->weights) + first * p->top * type_bytes(p->weights_type);
+    a.out = static_cast<unsigned char *>(p->out) + first * p->out_stride * type_bytes(p->out_type);
+    const dim3 groups((unsigned)((a.tokens * pieces + 3) / 4));
+    with_types(p->y_type, p->out_type, [&](auto y, auto o) { hipLaunchKernelGGL((lutkan_expert_combine_kernel<y, o>), groups, dim3(256), 0, s, a); });
+    if (int rc = check_launch(who)) return rc;
+  }
+  return LUTKAN_OK;
+}
+
+extern "C" int lutkan_expert_combine_backward(const lutkan_expert_combine_backward_args *p, void *hip_stream) {
+  const char *who = "lutkan_expert_combine_backward";
+  if (!p) return fail(LUTKAN_EINVAL, "%s: null arguments", who);
+  if (int rc = check_tokens(who, p->tokens, p->top, p->width, p->y_rows)) return rc;
+  if (!is_type(p->grad_type) || !is_type(p->y_type) || (p->weights && !is_type(p->weights_type))) return fail(LUTKAN_EINVAL, "%s: bad type", who);
+  if (!is_whole(p->places_bytes) || !is_whole(p->rows_bytes)) return fail(LUTKAN_EINVAL, "%s: rows and places are whole numbers of 4 or 8 bytes", who);
+  if ((p->weights != nullptr) != (p->grad_weights != nullptr) && p->tokens > 0) return fail(LUTKAN_EINVAL, "%s: weights and grad_weights come together", who);
+  if (p->tokens > 0 && (!p->grad || !p->places)) return fail(LUTKAN_EINVAL, "%s: null grad / places", who);
+  if (p->y_rows > 0 && (!p->rows || !p->grad_y || (p->weights && !p->y))) return fail(LUTKAN_EINVAL, "%s: null rows / grad_y / y", who);
+  if (p->grad_stride < 0 || (p->weights && p->y_stride < 0) || (p->y_rows > 0 && p->grad_y_stride < p->width)) return fail(LUTKAN_ESHAPE, "%s: a negative stride, or a row of grad_y that is longer than its stride", who);
+  if (std::max({p->grad_stride, p->weights ? p->y_stride : 0, p->grad_y_stride}) > INT32_MAX) return fail(LUTKAN_EUNSUPPORTED, "%s: row strides of at most 2^31 - 1", who);
+  BackwardArgs a;
+  a.grad = static_cast<const unsigned char *>(p->grad); a.y = static_cast<const unsigned char *>(p->y); a.weights = static_cast<const unsigned char *>(p->weights);
+  a.rows = p->rows; a.places = p->places; a.grad_y = static_cast<unsigned char *>(p->grad_y); a.grad_weights = static_cast<unsigned char *>(p->grad_weights);
+  a.y_rows = p->y_rows; a.tokens = p->tokens; a.grad_stride = (int32_t)p->grad_stride; a.y_stride = p->weights ? (int32_t)p->y_stride : 0; a.grad_y_stride = (int32_t)p->grad_y_stride;
+  a.top = p->top; a.width = p->width; a.weights_type = (int8_t)p->weights_type; a.rows_bytes = (int8_t)p->rows_bytes; a.places_bytes = (int8_t)p->places_bytes;
+  const int threads = 64 * std::min((p->width + 511) / 512, 16);
+  const int64_t groups = p->tokens + (p->y_rows + 63) / 64;
+  if (groups == 0) return LUTKAN_OK;
+  if (!lutkan::launch_holds(groups, threads)) return fail(LUTKAN_EUNSUPPORTED, "%s: too many tokens", who);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  with_types(p->grad_type, p->y_type, [&](auto g, auto y) { hipLaunchKernelGGL((lutkan_expert_combine_backward_kernel<g, y>), dim3((unsigned)groups), dim3(threads), 0, s, a); });
+  return check_launch(who);
+}
