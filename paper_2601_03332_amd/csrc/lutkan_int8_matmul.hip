@@ -157,14 +157,369 @@ int launch_direct(ProductArgs a, int64_t row_tiles, bool aligned, const char *wh
   return check_launch(who);
 }
 
+// Outputs of 32 rows x 32 columns, a lane's sixteen sums: columns 8 g + 4 h + e of row lane % 32, g < 4, h = lane / 32.  16-bit ones: the lane halves
+// of two column groups change places, so that a lane holds eight neighbouring outputs, 16 bytes.
+template <int TYPE>
+__device__ __forceinline__ void store_32x32(const ProductArgs &a, int64_t row, bool exists, int col0, int h, const f32x4 (&v)[4]) {
+  if constexpr (TYPE == LUTKAN_F32) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = col0 + 8 * g + 4 * h;
+      if (!exists || col >= a.n) continue;
+      unsigned char *to = a.y + (row * a.y_stride + col) * 4;
+      if (col + 4 <= a.n) { store_any(to, v[g]); continue; }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) if (col + e < a.n) store_any(to + 4 * e, v[g][e]);
+    }
+  } else {
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+      unsigned bits[2][4];
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bits[o][e] = TYPE == LUTKAN_F16 ? f16_bits(v[g + o][e]) : bf16_bits(v[g + o][e]);
+      const u32x2 low = __builtin_amdgcn_permlane32_swap(bits[0][0] | (bits[0][1] << 16), bits[1][0] | (bits[1][1] << 16), false, false);
+      const u32x2 high = __builtin_amdgcn_permlane32_swap(bits[0][2] | (bits[0][3] << 16), bits[1][2] | (bits[1][3] << 16), false, false);
+      const u32x4 eight{low[0], high[0], low[1], high[1]};
+      const int col = col0 + 8 * (g + h);
+      if (!exists || col >= a.n) continue;
+      unsigned char *to = a.y + (row * a.y_stride + col) * 2;
+      if (col + 8 <= a.n) { store_any(to, eight); continue; }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (col + e < a.n) store_any(to + 2 * e, (unsigned short)(eight[e >> 1] >> ((e & 1) * 16)));
+    }
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vector_loads() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4 << 14)); }      // vmcnt(N)
+
+// A tile of 32 TM WM rows x 32 TN WN columns for a work-group of KG teams of WM x WN waves, each wave 32 TM rows x 32 TN columns of it.  The teams
+// take the blocks of 128 k in turn; their sums meet in LDS.  A team's blocks go through LDS, in two buffers.  A row's eight 16-byte pieces lie in an
+// order that depends on the row (piece_place), so that the 16 rows that a read of 16 lanes takes lie in different banks.
+//   A block is multiplied in four steps of 32 k.  While one is, the next one's fragments are read, and the following block's copies go out; only the last
+//   step has to know that all waves have read the block and that the next one is there, and its fragments have been read before.
+//   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and offsets that fit 32 bits.
+//   Otherwise, and for a last block that is not whole, through registers.
+template <int TM, int TN, int WM, int WN, int KG>
+struct Tile {
+  static constexpr int kRows = 32 * TM * WM, kCols = 32 * TN * WN, kThreads = 64 * WM * WN, kStage = (kRows + kCols) * kScaleBlock;
+  static constexpr int kParts = KG > 1 ? (KG - 1) * kRows * kCols * 4 : 0;       // the sums of all teams but the one that adds them up
+  static constexpr int kLds = KG * 2 * kStage > kParts ? KG * 2 * kStage : kParts;
+  static_assert(kLds <= lutkan::kLdsPerWorkGroup, "LDS");
+};
+
+template <int TM, int TN, int WM, int WN, int KG, bool GROUPED, bool ASYNC>
+__global__ __launch_bounds__(64 * WM * WN * KG, TM * TN >= 16 ? 1 : WM * WN * KG >= 16 ? 4 : 2) void lutkan_int8_tiled_kernel(const ProductArgs a) {
+  using T = Tile<TM, TN, WM, WN, KG>;
+  constexpr int kRows = T::kRows, kCols = T::kCols, kWaves = WM * WN, kStage = T::kStage;
+  constexpr int kXCopies = kRows / 8 / kWaves, kWCopies = kCols / 8 / kWaves, kCopies = kXCopies + kWCopies;     // of 8 rows, for each wave
+  static_assert(kXCopies * 8 * kWaves == kRows && kWCopies * 8 * kWaves == kCols && kXCopies % 2 == 0 && kWCopies % 2 == 0, "copies in pairs");
+  extern __shared__ __align__(16) unsigned char s_tiles[];       // [team][buffer][rows of x, rows of the weight][128]
+  const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave_of_all / kWaves;
+  const int wave = wave_of_all % kWaves, wm = wave / WN, wn = wave % WN, h = lane >> 5;
+  // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, and in a run eight row tiles share a column
+  // tile before the next, so that what an XCD's work-groups read at a time meets in its L2.
+  const unsigned col_tiles = (a.n + kCols - 1) / kCols;
+  int col0 = 0;
+  const auto tile_of = [&](unsigned row_tiles) {                 // the row tile; sets the column
+    const unsigned tiles = row_tiles * col_tiles;
+    if (blockIdx.x >= tiles) return -1;
+    const unsigned xcd = blockIdx.x % 8, of_xcd = tiles / 8, more = tiles % 8;
+    const unsigned tile = xcd * of_xcd + min(xcd, more) + blockIdx.x / 8;
+    const unsigned band = tile / (8 * col_tiles), in_band = tile - band * 8 * col_tiles, high = min(8u, row_tiles - band * 8);
+    col0 = (int)(in_band / high) * kCols;
+    return (int)(band * 8 + in_band % high);
+  };
+  RowTile t;
+  if constexpr (GROUPED) {
+    t = grouped_tile<kRows>(a, tile_of);
+  } else {
+    t.first = (int64_t)tile_of(a.extent) * kRows;               // (the grid has as many work-groups as there are tiles)
+    t.end = min(t.first + kRows, (int64_t)a.rows);
+    t.group = 0;
+  }
+  if (t.end <= t.first) return;
+  i32x16 acc[TM][TN];
+#pragma unroll
+  for (int m = 0; m < TM; ++m)
+#pragma unroll
+    for (int n = 0; n < TN; ++n) acc[m][n] = i32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+  if (t.group >= 0) {
+    const unsigned char *w_tile = a.w + t.group * a.w_matrix_stride + (int64_t)col0 * a.w_stride;
+    const unsigned char *x_tile = GROUPED ? a.x : a.x + t.first * a.x_stride;
+    typedef std::conditional_t<ASYNC, unsigned, int64_t> offset_t;
+    offset_t x_from[kXCopies], w_from[kWCopies];                 // the rows that this lane's pieces come from
+    int piece_at[2];                                             // and the columns: place i of row r, the same for every 16 rows
+#pragma unroll
+    for (int c = 0; c < 2; ++c) piece_at[c] = piece_place(c * 8 + (lane >> 3), lane & 7) * 16;
+    const auto row_of = [&](int r) {                             // rows behind the last are the last again
+      const int64_t row = min(t.first + r, t.end - 1);
+      return GROUPED ? max(source_row<GROUPED>(a, row), (int64_t)0) : row - t.first;
+    };
+#pragma unroll
+    for (int c = 0; c < kXCopies; ++c) x_from[c] = (offset_t)(row_of((wave * kXCopies + c) * 8 + (lane >> 3)) * a.x_stride) + (ASYNC ? piece_at[c & 1] : 0);
+#pragma unroll
+    for (int c = 0; c < kWCopies; ++c) w_from[c] = (offset_t)((int64_t)min((wave * kWCopies + c) * 8 + (lane >> 3), a.n - 1 - col0) * a.w_stride) + (ASYNC ? piece_at[c & 1] : 0);
+    const int whole = a.k / kScaleBlock, own = (whole - team + KG - 1) / KG, steps = (whole + KG - 1) / KG;     // whole blocks: all, this team's, the first team's
+    unsigned char *const s_team = s_tiles + team * 2 * kStage;
+    const auto stage = [&](int step) { return s_team + (step & 1) * kStage; };
+    Piece<false> held[ASYNC ? 1 : kCopies];                      // (without ASYNC: rows at any address)
+    // Copy c of this team's block of a step: on its way into its buffer, or asked for until put() puts it there.
+    const auto ask = [&](int step, int c) {
+      const bool of_x = c < kXCopies;
+      const int cw = c - kXCopies;
+      const int64_t b = (int64_t)(step * KG + team) * kScaleBlock;
+      if constexpr (ASYNC) {
+        unsigned char *to = stage(step) + (of_x ? (wave * kXCopies + c) * 1024 : kRows * kScaleBlock + (wave * kWCopies + cw) * 1024);
+        copy16_global_to_lds_at((of_x ? x_tile : w_tile) + b, of_x ? x_from[c] : w_from[cw], to);
+      } else {
+        held[c].read((of_x ? x_tile + x_from[c] : w_tile + w_from[cw]) + (b + piece_at[c & 1]));
+      }
+    };
+    const auto put = [&](int step) {
+      if constexpr (!ASYNC) {
+        unsigned char *to = stage(step) + lane * 16;
+#pragma unroll
+        for (int c = 0; c < kXCopies; ++c) *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = held[c].get(low_bits(x_tile + x_from[c]));
+#pragma unroll
+        for (int c = 0; c < kWCopies; ++c) *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = held[kXCopies + c].get(low_bits(w_tile + w_from[c]));
+      }
+    };
+    // The last block, if it is not whole: this team's step `own`.
+    const auto put_end = [&]() {
+      unsigned char *to = stage(own) + lane * 16;
+      for (int c = 0; c < kXCopies; ++c)
+        *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = piece_at_end(x_tile + (x_from[c] - (ASYNC ? piece_at[c & 1] : 0)), whole * kScaleBlock + piece_at[c & 1], a.k);
+      for (int c = 0; c < kWCopies; ++c)
+        *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = piece_at_end(w_tile + (w_from[c] - (ASYNC ? piece_at[c & 1] : 0)), whole * kScaleBlock + piece_at[c & 1], a.k);
+    };
+    int at_piece[4];                                             // a lane's bytes of a 32-row subtile, by step of 32 k
+#pragma unroll
+    for (int q = 0; q < 4; ++q) at_piece[q] = (lane & 31) * kScaleBlock + piece_place(lane & 31, 2 * q + h) * 16;
+    u32x4 xf[2][TM], wf[2][TN];
+    // Fragment f of a step of 32 k, into buffer q & 1.
+    const auto read = [&](int step, int q, int f) {
+      const unsigned char *from = stage(step) + at_piece[q] + (f < TM ? (wm * TM + f) * 32 * kScaleBlock : (kRows + (wn * TN + f - TM) * 32) * kScaleBlock);
+      if (f < TM) xf[q & 1][f] = *reinterpret_cast<const u32x4 *>(from);
+      else wf[q & 1][f - TM] = *reinterpret_cast<const u32x4 *>(from);
+    };
+    constexpr int kFirst = kCopies / 2;                          // of a block's copies go out behind the barrier, the others a step later
+    // One step of 32 k: its products, and between them what the flags ask for.  READ: fragments of the next one; COPY: of the block's copies.
+    const auto multiply = [&](auto q_, auto read_, auto copy_, int read_step, int copy_step) {
+      constexpr int q = decltype(q_)::value, kReads = decltype(read_)::value ? TM + TN : 0;
+      constexpr int kAsk = !decltype(copy_)::value ? 0 : q == 3 ? kFirst : q == 0 ? kCopies - kFirst : 0, kOps = kReads + kAsk, kAll = TM * TN;
+#pragma unroll
+      for (int i = 0; i < kAll; ++i) {
+#pragma unroll
+        for (int o = i * kOps / kAll; o < (i + 1) * kOps / kAll; ++o) {
+          if (o < kReads) read(read_step, (q + 1) & 3, o);
+          else ask(copy_step, o - kReads + (q == 0 ? kFirst : 0));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        acc[i / TN][i % TN] = product_32x32(wf[q & 1][i % TN], xf[q & 1][i / TN], acc[i / TN][i % TN]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const auto block = [&](int step, auto next_, auto after_) {  // next: there is another block; after: and one behind it
+      multiply(std::integral_constant<int, 0>(), Yes(), next_, step, step + 1);
+      multiply(std::integral_constant<int, 1>(), Yes(), No(), step, 0);
+      multiply(std::integral_constant<int, 2>(), Yes(), No(), step, 0);
+      wait_all_vector_loads();
+      if constexpr (decltype(next_)::value) put(step + 1);
+      lds_barrier();                                             // the next block is there, and nobody reads this one any more
+      multiply(std::integral_constant<int, 3>(), next_, after_, step + 1, step + 2);
+    };
+    if (own > 0) {
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) ask(0, c);
+      put(0);
+    }
+    if (own > 1) {
+#pragma unroll
+      for (int c = 0; c < kFirst; ++c) ask(1, c);
+      if constexpr (ASYNC) wait_vector_loads<kFirst>();
+    } else {
+      wait_all_vector_loads();
+    }
+    lds_barrier();
+    if (own > 0) {
+#pragma unroll
+      for (int f = 0; f < TM + TN; ++f) read(0, 0, f);
+    }
+    int step = 0;
+    for (; step + 2 < own; ++step) block(step, Yes(), Yes());
+    if (step + 1 < own) block(step++, Yes(), No());
+    if (step < own) block(step++, No(), No());
+    for (; step < steps; ++step) lds_barrier();                  // (a team with a block less than the first)
+    if (whole < a.k_blocks()) {
+      const bool mine = whole % KG == team;
+      if (mine) put_end();                                       // (into a buffer that nobody reads since the last barrier)
+      lds_barrier();
+      if (mine) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+          for (int f = 0; f < TM + TN; ++f) read(own, q, f);
+#pragma unroll
+          for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] = product_32x32(wf[q & 1][i % TN], xf[q & 1][i / TN], acc[i / TN][i % TN]);
+        }
+      }
+    }
+    if constexpr (KG > 1) {
+      lds_barrier();                                             // nobody reads the buffers any more
+      i32x4 *parts = reinterpret_cast<i32x4 *>(s_tiles);         // [team - 1][wave][m][n][quarter][lane]
+      const auto place = [&](int of, int m, int n, int g) { return ((((of * kWaves + wave) * TM + m) * TN + n) * 4 + g) * 64 + lane; };
+      if (team > 0) {
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+          for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) parts[place(team - 1, m, n, g)] = i32x4{acc[m][n][4 * g], acc[m][n][4 * g + 1], acc[m][n][4 * g + 2], acc[m][n][4 * g + 3]};
+      }
+      lds_barrier();
+      if (team > 0) return;
+#pragma unroll
+      for (int m = 0; m < TM; ++m)
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            for (int o = 0; o < KG - 1; ++o) {
+              const i32x4 part = parts[place(o, m, n, g)];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[m][n][4 * g + e] += part[e];
+            }
+    }
+  }
+  if (KG > 1 && team > 0) return;
+  int64_t from[TM];
+  float xs[TM];
+  bool fine = true;
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    const int64_t row = t.first + (wm * TM + m) * 32 + (lane & 31);
+    from[m] = t.group < 0 ? -1 : source_row<GROUPED>(a, min(row, t.end - 1));
+    xs[m] = from[m] >= 0 ? a.x_scales[from[m] * a.x_scales_stride] : 1.0f;
+    fine = fine && ordinary(xs[m]);
+  }
+#pragma unroll
+  for (int n = 0; n < TN; ++n) {
+    const int col = col0 + (wn * TN + n) * 32;
+    if (col >= a.n) break;
+    f32x4 ws[4];
+    bool ok = fine;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      ws[g] = weight_scales(a, max(t.group, 0), col + 8 * g + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ok = ok && ordinary(ws[g][e]);
+    }
+    const bool exact = !__all(ok);
+#pragma unroll
+    for (int m = 0; m < TM; ++m) {
+      const int64_t row = t.first + (wm * TM + m) * 32 + (lane & 31);
+      f32x4 v[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        v[g] = scaled(i32x4{acc[m][n][4 * g], acc[m][n][4 * g + 1], acc[m][n][4 * g + 2], acc[m][n][4 * g + 3]}, xs[m], ws[g], exact);
+        if (from[m] < 0) v[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+      switch (a.y_type) {
+        case LUTKAN_F32: store_32x32<LUTKAN_F32>(a, row, row < t.end, col, h, v); break;
+        case LUTKAN_F16: store_32x32<LUTKAN_F16>(a, row, row < t.end, col, h, v); break;
+        default: store_32x32<LUTKAN_BF16>(a, row, row < t.end, col, h, v); break;
+      }
+    }
+  }
+}
+
+template <int TM, int TN, int WM, int WN, int KG, bool GROUPED, bool ASYNC>
+int launch_tiles_as(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
+  using T = Tile<TM, TN, WM, WN, KG>;
+  static LdsCap cap;
+  a.extent = (int32_t)row_tiles;
+  const auto kernel = lutkan_int8_tiled_kernel<TM, TN, WM, WN, KG, GROUPED, ASYNC>;
+  if (int rc = raise_lds_cap(kernel, &cap, who)) return rc;
+  lutkan::plan_note("int8_tiled rows=%d columns=%d teams=%d%s; ", T::kRows, T::kCols, KG, ASYNC ? " async" : "");
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * ((a.n + T::kCols - 1) / T::kCols))), dim3(T::kThreads * KG), T::kLds, s, a);
+  return check_launch(who);
+}
+
+template <int TM, int TN, int WM, int WN, int KG, bool GROUPED>
+int launch_tiles(const ProductArgs &a, int64_t row_tiles, bool async, const char *who, hipStream_t s) {
+  return async ? launch_tiles_as<TM, TN, WM, WN, KG, GROUPED, true>(a, row_tiles, who, s) : launch_tiles_as<TM, TN, WM, WN, KG, GROUPED, false>(a, row_tiles, who, s);
+}
+
+inline double direct_price(double row_tiles, double rows_of_tile, int columns, const ProductArgs &a) {
+  const double work_groups = row_tiles * ((a.n + columns - 1) / columns);
+  return work_groups * (rows_of_tile + columns) * a.k / (9e6 * std::min(1.0, work_groups / 256));
+}
+inline double tiled_price(double tiles, int slots, double one, double all, double ends, double steps, bool guess) {
+  if (guess && slots > 1 && tiles > 256) return std::max(1.0, tiles / (256 * slots)) * (steps * all + ends);
+  const double full = std::floor(tiles / (256 * slots)), rest = tiles - full * 256 * slots;
+  return full * (steps * all + ends) + (rest > 0 ? steps * (rest <= 256 ? one : all) + ends : 0);
+}
+
 template <bool GROUPED>
 int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   const int64_t groups = GROUPED ? a.groups : 1;
   const auto tiles = [&](int height) {                           // no routing has more
     return GROUPED ? a.rows / height + std::min<int64_t>(groups + 1, a.rows) : ((int64_t)a.rows + height - 1) / height;
   };
+  const auto likely_tiles = [&](int height) {                    // of a routing of some spread: a group's last tile is half empty
+    if (!GROUPED) return (double)tiles(height);
+    const double some = (double)std::min<int64_t>(groups, a.rows), each = (double)a.rows / some;
+    return some * std::max(1.0, each / height + (each > 1 ? 0.6 : 0.0));
+  };
   lutkan::plan_clear();
-  return launch_direct<2, 2, GROUPED>(a, tiles(32), rows_aligned(a), who, s);
+  const bool aligned = rows_aligned(a), async = aligned && copies_fit<GROUPED>(a);
+  const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows);
+  const double end_block = a.k % kScaleBlock ? 2.5 : 0;          // (read, put and multiplied behind the others)
+  const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
+    const double step = async ? 1 : side == 64 ? 1.75 : 1.5;     // (through registers a step waits longer)
+    return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one * step, all * step, ends + end_block, std::ceil(a.k / kScaleBlock / (double)teams), GROUPED);
+  };
+  enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kKernels };
+  double price[kKernels];
+  price[kDirect16x16] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 16, a);
+  price[kDirect16x32] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 32, a);
+  price[kDirect32x32] = direct_price(likely_tiles(32), std::min(32.0, likely_rows), 32, a);
+  constexpr double kSearch = GROUPED ? 2 : 0;                    // for the group, before a small tile's few steps
+  price[kTiled64x4] = tiled(64, 1, 0.62, 1.0, 1 + kSearch, 4);
+  price[kTiled64x2] = tiled(64, 2, 0.36, 0.85, 1 + kSearch, 2);
+  price[kTiled128x2] = tiled(128, 1, 1.0, 1.0, 5, 2);
+  price[kTiled128] = tiled(128, 2, 0.65, 1.08, 2, 1);
+  price[kTiled256] = tiled(256, 1, 1.3, 1.3, 6, 1);
+  if (GROUPED)                                                   // (weights that few rows share come from memory)
+    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.7;
+  if (!aligned)                                                  // (five dwords for every four)
+    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 2;
+  if (!async) price[kTiled256] = HUGE_VAL;                       // (its sums leave no registers to copy through)
+  if (tiles(16) > 65535) price[kDirect16x16] = price[kDirect16x32] = HUGE_VAL;
+  if (tiles(32) > 65535) price[kDirect32x32] = HUGE_VAL;
+  const auto beyond_a_launch = [&](int side, int threads) { return !lutkan::launch_holds(tiles(side) * ((a.n + side - 1) / side), threads); };
+  if (beyond_a_launch(64, 1024)) price[kTiled64x4] = HUGE_VAL;
+  if (beyond_a_launch(64, 512)) price[kTiled64x2] = HUGE_VAL;
+  if (beyond_a_launch(128, 512)) price[kTiled128x2] = HUGE_VAL;
+  if (beyond_a_launch(128, 256)) price[kTiled128] = HUGE_VAL;
+  if (beyond_a_launch(256, 256)) price[kTiled256] = HUGE_VAL;
+  const int pick = (int)(std::min_element(price, price + kKernels) - price);
+  if (price[pick] == HUGE_VAL) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
+  switch (pick) {
+    case kDirect16x16: return launch_direct<1, 1, GROUPED>(a, tiles(16), aligned, who, s);
+    case kDirect16x32: return launch_direct<1, 2, GROUPED>(a, tiles(16), aligned, who, s);
+    case kDirect32x32: return launch_direct<2, 2, GROUPED>(a, tiles(32), aligned, who, s);
+    case kTiled64x4: return launch_tiles<1, 1, 2, 2, 4, GROUPED>(a, tiles(64), async, who, s);
+    case kTiled64x2: return launch_tiles<1, 1, 2, 2, 2, GROUPED>(a, tiles(64), async, who, s);
+    case kTiled128x2: return launch_tiles<2, 2, 2, 2, 2, GROUPED>(a, tiles(128), async, who, s);
+    case kTiled256: return launch_tiles_as<4, 4, 2, 2, 1, GROUPED, true>(a, tiles(256), who, s);
+    default: return launch_tiles<2, 2, 2, 2, 1, GROUPED>(a, tiles(128), async, who, s);
+  }
 }
 
 int check_product(const lutkan_matmul_fp8_args *p, const char *who, ProductArgs *a) {
