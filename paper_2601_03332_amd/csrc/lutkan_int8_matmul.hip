@@ -157,38 +157,106 @@ int launch_direct(ProductArgs a, int64_t row_tiles, bool aligned, const char *wh
   return check_launch(who);
 }
 
-// Outputs of 32 rows x 32 columns, a lane's sixteen sums: columns 8 g + 4 h + e of row lane % 32, g < 4, h = lane / 32.  16-bit ones: the lane halves
-// of two column groups change places, so that a lane holds eight neighbouring outputs, 16 bytes.
+// The outputs of a wave's 32 TM rows x 32 TN columns.  A lane's sixteen sums of 32 x 32 are columns 8 g + 4 h + e of row lane % 32 (g < 4, h = lane / 32, e < 4):
+// 32 rows at a time change places through LDS, so that neighbouring lanes hold neighbouring outputs, 16 bytes each, and a store covers whole
+// rows of the tile.  (Stored from where they lie the code is as long as the sums are many: 16000 instructions for 128 x 128, which took 24 us to fetch.)
+constexpr int dump_pitch(int TN) { return 32 * TN * 4 + 16; }    // bytes of a row there
+constexpr int dump_bytes(int TN) { return 32 * dump_pitch(TN); }
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <int TYPE>
-__device__ __forceinline__ void store_32x32(const ProductArgs &a, int64_t row, bool exists, int col0, int h, const f32x4 (&v)[4]) {
+__device__ __forceinline__ unsigned two_outputs(float a, float b) {
+  if constexpr (TYPE == LUTKAN_BF16) return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b});
+  else return f16_bits(a) | (f16_bits(b) << 16);
+}
+
+// Four (32 bits) or eight (16 bits) neighbouring outputs of a row.
+template <int TYPE, int N>
+__device__ __forceinline__ void store_some(const ProductArgs &a, int64_t row, int col, const f32x4 (&v)[N]) {
   if constexpr (TYPE == LUTKAN_F32) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int col = col0 + 8 * g + 4 * h;
-      if (!exists || col >= a.n) continue;
-      unsigned char *to = a.y + (row * a.y_stride + col) * 4;
-      if (col + 4 <= a.n) { store_any(to, v[g]); continue; }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) if (col + e < a.n) store_any(to + 4 * e, v[g][e]);
-    }
+    store_outputs(a, row, col, v[0]);
   } else {
+    unsigned char *to = a.y + (row * a.y_stride + col) * 2;
+    const u32x4 eight{two_outputs<TYPE>(v[0][0], v[0][1]), two_outputs<TYPE>(v[0][2], v[0][3]), two_outputs<TYPE>(v[1][0], v[1][1]), two_outputs<TYPE>(v[1][2], v[1][3])};
+    if (col + 8 <= a.n) { store_any(to, eight); return; }
 #pragma unroll
-    for (int g = 0; g < 4; g += 2) {
-      unsigned bits[2][4];
+    for (int e = 0; e < 8; ++e) if (col + e < a.n) store_any(to + 2 * e, (unsigned short)(eight[e >> 1] >> ((e & 1) * 16)));
+  }
+}
+
+template <int TYPE, int TM, int TN, bool GROUPED>
+__device__ __forceinline__ void store_wave(const ProductArgs &a, const RowTile &t, const i32x16 (&acc)[TM][TN], int64_t row0, int col0, unsigned char *dump) {
+  constexpr int kCols = TYPE == LUTKAN_F32 ? 4 : 8, kLanes = 32 * TN / kCols, kRows = 64 / kLanes;       // columns of a lane, lanes of a row, rows at a time
+  const int lane = threadIdx.x & 63, col = col0 + lane % kLanes * kCols;
+  const int64_t last = t.end - 1;
+  float xs[TM];                                                  // of row 32 m + lane % 32; 0: a row of zeros
+  bool fine = true;
 #pragma unroll
-      for (int o = 0; o < 2; ++o)
+  for (int m = 0; m < TM; ++m) {
+    const int64_t from = t.group < 0 ? -1 : source_row<GROUPED>(a, min(row0 + 32 * m + (lane & 31), last));
+    xs[m] = from >= 0 ? a.x_scales[from * a.x_scales_stride] : 0.0f;
+    fine = fine && (from < 0 || ordinary(xs[m]));
+  }
+  f32x4 ws[kCols / 4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bits[o][e] = TYPE == LUTKAN_F16 ? f16_bits(v[g + o][e]) : bf16_bits(v[g + o][e]);
-      const u32x2 low = __builtin_amdgcn_permlane32_swap(bits[0][0] | (bits[0][1] << 16), bits[1][0] | (bits[1][1] << 16), false, false);
-      const u32x2 high = __builtin_amdgcn_permlane32_swap(bits[0][2] | (bits[0][3] << 16), bits[1][2] | (bits[1][3] << 16), false, false);
-      const u32x4 eight{low[0], high[0], low[1], high[1]};
-      const int col = col0 + 8 * (g + h);
-      if (!exists || col >= a.n) continue;
-      unsigned char *to = a.y + (row * a.y_stride + col) * 2;
-      if (col + 8 <= a.n) { store_any(to, eight); continue; }
+  for (int i = 0; i < kCols / 4; ++i) {
+    ws[i] = weight_scales(a, max(t.group, 0), col + 4 * i);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (col + e < a.n) store_any(to + 2 * e, (unsigned short)(eight[e >> 1] >> ((e & 1) * 16)));
+    for (int e = 0; e < 4; ++e) fine = fine && ordinary(ws[i][e]);
+  }
+  const bool exact = !__all(fine);                               // (then the sums change places, and not their products with xs)
+  unsigned char *const to = dump + (lane & 31) * dump_pitch(TN) + (lane >> 5) * 16;
+  const unsigned char *const from = dump + lane / kLanes * dump_pitch(TN) + lane % kLanes * kCols * 4;
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    const bool none = xs[m] == 0.0f;
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        i32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float product = none ? 0.0f : (float)acc[m][n][4 * g + e] * xs[m];
+          v[e] = exact ? acc[m][n][4 * g + e] : (int)__float_as_uint(product);
+        }
+        *reinterpret_cast<i32x4 *>(to + (32 * n + 8 * g) * 4) = v;
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (!exact) {
+      constexpr int kParts = 32 / kRows < 4 ? 32 / kRows : 4;
+#pragma unroll 1
+      for (int r0 = 0; r0 < 32; r0 += kParts * kRows) {
+        f32x4 v[kParts][kCols / 4];
+#pragma unroll
+        for (int o = 0; o < kParts; ++o)
+#pragma unroll
+          for (int i = 0; i < kCols / 4; ++i) v[o][i] = *reinterpret_cast<const f32x4 *>(from + (r0 + o * kRows) * dump_pitch(TN) + 16 * i);
+#pragma unroll
+        for (int o = 0; o < kParts; ++o) {
+#pragma unroll
+          for (int i = 0; i < kCols / 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[o][i][e] *= ws[i][e];
+          const int64_t row = row0 + 32 * m + r0 + o * kRows + lane / kLanes;
+          if (row <= last && col < a.n) store_some<TYPE>(a, row, col, v[o]);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int r0 = 0; r0 < 32; r0 += kRows) {
+        const int64_t row = row0 + 32 * m + r0 + lane / kLanes, source = t.group < 0 ? -1 : source_row<GROUPED>(a, min(row, last));
+        const float x_scale = source < 0 ? 0.0f : a.x_scales[source * a.x_scales_stride];
+        f32x4 v[kCols / 4];
+#pragma unroll
+        for (int i = 0; i < kCols / 4; ++i) {
+          v[i] = scaled(*reinterpret_cast<const i32x4 *>(from + r0 * dump_pitch(TN) + 16 * i), x_scale, ws[i], true);
+          if (source < 0) v[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        if (row <= last && col < a.n) store_some<TYPE>(a, row, col, v);
+      }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the next rows come behind the reads of these
   }
 }
 
@@ -196,27 +264,29 @@ template <int N>
 __device__ __forceinline__ void wait_vector_loads() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4 << 14)); }      // vmcnt(N)
 
 // A tile of 32 TM WM rows x 32 TN WN columns for a work-group of KG teams of WM x WN waves, each wave 32 TM rows x 32 TN columns of it.  The teams
-// take the blocks of 128 k in turn; their sums meet in LDS.  A team's blocks go through LDS, in two buffers.  A row's eight 16-byte pieces lie in an
-// order that depends on the row (piece_place), so that the 16 rows that a read of 16 lanes takes lie in different banks.
-//   A block is multiplied in four steps of 32 k.  While one is, the next one's fragments are read, and the following block's copies go out; only the last
+// take the blocks of k in turn; their sums meet in LDS.  A team's blocks go through LDS, in several buffers.  A row's 16-byte pieces lie in an
+// order that depends on the row (piece_at), so that the 16 rows that a read of 16 lanes takes lie in different banks.
+//   A block is multiplied in steps of 32 k.  While one is, the next one's fragments are read, and copies of a later block go out; only the last
 //   step has to know that all waves have read the block and that the next one is there, and its fragments have been read before.
-//   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and offsets that fit 32 bits.
-//   Otherwise, and for a last block that is not whole, through registers.
-template <int TM, int TN, int WM, int WN, int KG>
+//   ASYNC: the pieces go from global memory to LDS without passing through registers: needs rows at dword addresses and offsets that fit 32 bits.  Blocks
+//   of 64 k in five buffers: four are on their way while one is multiplied.
+//   Otherwise, and for a last block that is not whole, through registers: blocks of 128 k in two buffers.
+template <int TM, int TN, int WM, int WN, int KG, bool ASYNC>
 struct Tile {
-  static constexpr int kRows = 32 * TM * WM, kCols = 32 * TN * WN, kThreads = 64 * WM * WN, kStage = (kRows + kCols) * kScaleBlock;
+  static constexpr int kRows = 32 * TM * WM, kCols = 32 * TN * WN, kThreads = 64 * WM * WN;
+  static constexpr int kBlock = ASYNC ? 64 : 128, kStages = ASYNC ? 5 : 2, kStage = (kRows + kCols) * kBlock;
   static constexpr int kParts = KG > 1 ? (KG - 1) * kRows * kCols * 4 : 0;       // the sums of all teams but the one that adds them up
-  static constexpr int kLds = KG * 2 * kStage > kParts ? KG * 2 * kStage : kParts;
+  static constexpr int kLds = std::max(KG * kStages * kStage, kParts + WM * WN * dump_bytes(TN));
   static_assert(kLds <= lutkan::kLdsPerWorkGroup, "LDS");
 };
 
 template <int TM, int TN, int WM, int WN, int KG, bool GROUPED, bool ASYNC>
 __global__ __launch_bounds__(64 * WM * WN * KG, TM * TN >= 16 ? 1 : WM * WN * KG >= 16 ? 4 : 2) void lutkan_int8_tiled_kernel(const ProductArgs a) {
-  using T = Tile<TM, TN, WM, WN, KG>;
-  constexpr int kRows = T::kRows, kCols = T::kCols, kWaves = WM * WN, kStage = T::kStage;
-  constexpr int kXCopies = kRows / 8 / kWaves, kWCopies = kCols / 8 / kWaves, kCopies = kXCopies + kWCopies;     // of 8 rows, for each wave
-  static_assert(kXCopies * 8 * kWaves == kRows && kWCopies * 8 * kWaves == kCols && kXCopies % 2 == 0 && kWCopies % 2 == 0, "copies in pairs");
-  extern __shared__ __align__(16) unsigned char s_tiles[];       // [team][buffer][rows of x, rows of the weight][128]
+  using T = Tile<TM, TN, WM, WN, KG, ASYNC>;
+  constexpr int kRows = T::kRows, kCols = T::kCols, kWaves = WM * WN, kBlock = T::kBlock, kStages = T::kStages, kStage = T::kStage, kSteps = kBlock / 32, kPieces = kBlock / 16;
+  constexpr int kCopyRows = 1024 / kBlock, kXCopies = kRows / kCopyRows / kWaves, kWCopies = kCols / kCopyRows / kWaves, kCopies = kXCopies + kWCopies;     // for each wave
+  static_assert(kXCopies * kCopyRows * kWaves == kRows && kWCopies * kCopyRows * kWaves == kCols && 16 % kCopyRows == 0 && kXCopies * kCopyRows % 16 == 0 && kWCopies * kCopyRows % 16 == 0, "copies");
+  extern __shared__ __align__(16) unsigned char s_tiles[];       // [team][buffer][rows of x, rows of the weight][kBlock]
   const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave_of_all / kWaves;
   const int wave = wave_of_all % kWaves, wm = wave / WN, wn = wave % WN, h = lane >> 5;
   // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, and in a run eight row tiles share a column
@@ -247,123 +317,148 @@ __global__ __launch_bounds__(64 * WM * WN * KG, TM * TN >= 16 ? 1 : WM * WN * KG
 #pragma unroll
     for (int n = 0; n < TN; ++n) acc[m][n] = i32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   if (t.group >= 0) {
-    const unsigned char *w_tile = a.w + t.group * a.w_matrix_stride + (int64_t)col0 * a.w_stride;
-    const unsigned char *x_tile = GROUPED ? a.x : a.x + t.first * a.x_stride;
+    const auto uniform = [](const unsigned char *p) {            // (the copies take it from scalar registers)
+      const uint64_t at = reinterpret_cast<uint64_t>(p);
+      const unsigned high = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32)), low = __builtin_amdgcn_readfirstlane((unsigned)at);     // (unsigned: the builtin's result is signed)
+      return reinterpret_cast<const unsigned char *>((uint64_t)high << 32 | low);
+    };
+    const unsigned char *w_tile = uniform(a.w + t.group * a.w_matrix_stride + (int64_t)col0 * a.w_stride);
+    const unsigned char *x_tile = uniform(GROUPED ? a.x : a.x + t.first * a.x_stride);
+    // Piece `piece` of row `row` lies at this place of the row's kPieces (its own inverse).
+    const auto piece_at = [](int row, int piece) { return piece ^ (row / (16 / kPieces) & (kPieces - 1)); };
+    const int copy_row = lane / kPieces;                         // a lane's row of a copy, and the columns of its piece: the same for every 16 rows
+    const auto copy_from = [&](int c) { return piece_at(c * kCopyRows + copy_row, lane % kPieces) * 16; };
     typedef std::conditional_t<ASYNC, unsigned, int64_t> offset_t;
     offset_t x_from[kXCopies], w_from[kWCopies];                 // the rows that this lane's pieces come from
-    int piece_at[2];                                             // and the columns: place i of row r, the same for every 16 rows
-#pragma unroll
-    for (int c = 0; c < 2; ++c) piece_at[c] = piece_place(c * 8 + (lane >> 3), lane & 7) * 16;
     const auto row_of = [&](int r) {                             // rows behind the last are the last again
       const int64_t row = min(t.first + r, t.end - 1);
       return GROUPED ? max(source_row<GROUPED>(a, row), (int64_t)0) : row - t.first;
     };
 #pragma unroll
-    for (int c = 0; c < kXCopies; ++c) x_from[c] = (offset_t)(row_of((wave * kXCopies + c) * 8 + (lane >> 3)) * a.x_stride) + (ASYNC ? piece_at[c & 1] : 0);
+    for (int c = 0; c < kXCopies; ++c) x_from[c] = (offset_t)(row_of((wave * kXCopies + c) * kCopyRows + copy_row) * a.x_stride) + (ASYNC ? copy_from(c) : 0);
 #pragma unroll
-    for (int c = 0; c < kWCopies; ++c) w_from[c] = (offset_t)((int64_t)min((wave * kWCopies + c) * 8 + (lane >> 3), a.n - 1 - col0) * a.w_stride) + (ASYNC ? piece_at[c & 1] : 0);
-    const int whole = a.k / kScaleBlock, own = (whole - team + KG - 1) / KG, steps = (whole + KG - 1) / KG;     // whole blocks: all, this team's, the first team's
-    unsigned char *const s_team = s_tiles + team * 2 * kStage;
-    const auto stage = [&](int step) { return s_team + (step & 1) * kStage; };
+    for (int c = 0; c < kWCopies; ++c) w_from[c] = (offset_t)((int64_t)min((wave * kWCopies + c) * kCopyRows + copy_row, a.n - 1 - col0) * a.w_stride) + (ASYNC ? copy_from(c) : 0);
+    const int whole = a.k / kBlock, own = (whole - team + KG - 1) / KG, blocks = (whole + KG - 1) / KG;     // whole blocks: all, this team's, the first team's
+    unsigned char *const s_team = s_tiles + team * (kStages * kStage);
+    const auto stage = [&](int block) { return s_team + block % kStages * kStage; };
     Piece<false> held[ASYNC ? 1 : kCopies];                      // (without ASYNC: rows at any address)
-    // Copy c of this team's block of a step: on its way into its buffer, or asked for until put() puts it there.
-    const auto ask = [&](int step, int c) {
+    // Copy c of this team's block: on its way into its buffer, or asked for until put() puts it there.
+    const auto ask = [&](int block, unsigned char *to, int c) {
       const bool of_x = c < kXCopies;
       const int cw = c - kXCopies;
-      const int64_t b = (int64_t)(step * KG + team) * kScaleBlock;
-      if constexpr (ASYNC) {
-        unsigned char *to = stage(step) + (of_x ? (wave * kXCopies + c) * 1024 : kRows * kScaleBlock + (wave * kWCopies + cw) * 1024);
-        copy16_global_to_lds_at((of_x ? x_tile : w_tile) + b, of_x ? x_from[c] : w_from[cw], to);
-      } else {
-        held[c].read((of_x ? x_tile + x_from[c] : w_tile + w_from[cw]) + (b + piece_at[c & 1]));
-      }
+      const int64_t k0 = (int64_t)(block * KG + team) * kBlock;
+      if constexpr (ASYNC) copy16_global_to_lds_at((of_x ? x_tile : w_tile) + k0, of_x ? x_from[c] : w_from[cw], to + (of_x ? (wave * kXCopies + c) * 1024 : kRows * kBlock + (wave * kWCopies + cw) * 1024));
+      else held[c].read((of_x ? x_tile + x_from[c] : w_tile + w_from[cw]) + (k0 + copy_from(of_x ? c : cw)));
     };
-    const auto put = [&](int step) {
+    const auto put = [&](int block) {
       if constexpr (!ASYNC) {
-        unsigned char *to = stage(step) + lane * 16;
+        unsigned char *to = stage(block) + lane * 16;
 #pragma unroll
         for (int c = 0; c < kXCopies; ++c) *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = held[c].get(low_bits(x_tile + x_from[c]));
 #pragma unroll
-        for (int c = 0; c < kWCopies; ++c) *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = held[kXCopies + c].get(low_bits(w_tile + w_from[c]));
+        for (int c = 0; c < kWCopies; ++c) *reinterpret_cast<u32x4 *>(to + kRows * kBlock + (wave * kWCopies + c) * 1024) = held[kXCopies + c].get(low_bits(w_tile + w_from[c]));
       }
     };
-    // The last block, if it is not whole: this team's step `own`.
+    // The last block, if it is not whole: this team's block `own`.
     const auto put_end = [&]() {
       unsigned char *to = stage(own) + lane * 16;
       for (int c = 0; c < kXCopies; ++c)
-        *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = piece_at_end(x_tile + (x_from[c] - (ASYNC ? piece_at[c & 1] : 0)), whole * kScaleBlock + piece_at[c & 1], a.k);
+        *reinterpret_cast<u32x4 *>(to + (wave * kXCopies + c) * 1024) = piece_at_end(x_tile + (x_from[c] - (ASYNC ? copy_from(c) : 0)), whole * kBlock + copy_from(c), a.k);
       for (int c = 0; c < kWCopies; ++c)
-        *reinterpret_cast<u32x4 *>(to + kRows * kScaleBlock + (wave * kWCopies + c) * 1024) = piece_at_end(w_tile + (w_from[c] - (ASYNC ? piece_at[c & 1] : 0)), whole * kScaleBlock + piece_at[c & 1], a.k);
+        *reinterpret_cast<u32x4 *>(to + kRows * kBlock + (wave * kWCopies + c) * 1024) = piece_at_end(w_tile + (w_from[c] - (ASYNC ? copy_from(c) : 0)), whole * kBlock + copy_from(c), a.k);
     };
-    int at_piece[4];                                             // a lane's bytes of a 32-row subtile, by step of 32 k
+    int at_piece[kSteps];                                        // a lane's bytes of a 32-row subtile, by step of 32 k
 #pragma unroll
-    for (int q = 0; q < 4; ++q) at_piece[q] = (lane & 31) * kScaleBlock + piece_place(lane & 31, 2 * q + h) * 16;
+    for (int q = 0; q < kSteps; ++q) at_piece[q] = (lane & 31) * kBlock + piece_at(lane & 31, 2 * q + h) * 16;
     u32x4 xf[2][TM], wf[2][TN];
-    // Fragment f of a step of 32 k, into buffer q & 1.
-    const auto read = [&](int step, int q, int f) {
-      const unsigned char *from = stage(step) + at_piece[q] + (f < TM ? (wm * TM + f) * 32 * kScaleBlock : (kRows + (wn * TN + f - TM) * 32) * kScaleBlock);
+    // Fragment f of step q of a block, into buffer q & 1.
+    const auto read = [&](const unsigned char *of, int q, int f) {
+      const unsigned char *from = of + at_piece[q] + (f < TM ? (wm * TM + f) * 32 * kBlock : (kRows + (wn * TN + f - TM) * 32) * kBlock);
       if (f < TM) xf[q & 1][f] = *reinterpret_cast<const u32x4 *>(from);
       else wf[q & 1][f - TM] = *reinterpret_cast<const u32x4 *>(from);
     };
-    constexpr int kFirst = kCopies / 2;                          // of a block's copies go out behind the barrier, the others a step later
-    // One step of 32 k: its products, and between them what the flags ask for.  READ: fragments of the next one; COPY: of the block's copies.
-    const auto multiply = [&](auto q_, auto read_, auto copy_, int read_step, int copy_step) {
-      constexpr int q = decltype(q_)::value, kReads = decltype(read_)::value ? TM + TN : 0;
-      constexpr int kAsk = !decltype(copy_)::value ? 0 : q == 3 ? kFirst : q == 0 ? kCopies - kFirst : 0, kOps = kReads + kAsk, kAll = TM * TN;
+    constexpr int kFirst = kCopies / 2, kLast = kSteps - 1;      // of a block's copies go out behind the barrier, the others a step later
+    // Step q: its products, and between them READS fragments of the next step and ASKS copies of a block, from copy `first_ask` on.
+    const auto multiply = [&](auto q_, auto reads_, auto asks_, const unsigned char *read_from, int ask_block, int first_ask) {
+      constexpr int q = decltype(q_)::value, kReads = decltype(reads_)::value, kOps = kReads + decltype(asks_)::value, kAll = TM * TN;
+      unsigned char *const to = kOps > kReads ? stage(ask_block) : nullptr;
 #pragma unroll
       for (int i = 0; i < kAll; ++i) {
 #pragma unroll
         for (int o = i * kOps / kAll; o < (i + 1) * kOps / kAll; ++o) {
-          if (o < kReads) read(read_step, (q + 1) & 3, o);
-          else ask(copy_step, o - kReads + (q == 0 ? kFirst : 0));
+          if (o < kReads) read(read_from, (q + 1) % kSteps, o);
+          else ask(ask_block, to, first_ask + o - kReads);
         }
         __builtin_amdgcn_sched_barrier(0);
         acc[i / TN][i % TN] = product_32x32(wf[q & 1][i % TN], xf[q & 1][i / TN], acc[i / TN][i % TN]);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    using Yes = std::true_type;
-    using No = std::false_type;
-    const auto block = [&](int step, auto next_, auto after_) {  // next: there is another block; after: and one behind it
-      multiply(std::integral_constant<int, 0>(), Yes(), next_, step, step + 1);
-      multiply(std::integral_constant<int, 1>(), Yes(), No(), step, 0);
-      multiply(std::integral_constant<int, 2>(), Yes(), No(), step, 0);
-      wait_all_vector_loads();
-      if constexpr (decltype(next_)::value) put(step + 1);
+    // A block with `after` more behind it, at most kStages of which matter: of those, the next one has to be there at its last step, the copies of the
+    // last one in flight go out in two parts.
+    const auto multiply_block = [&](int block, auto after_) {
+      constexpr int kAfter = decltype(after_)::value, kAhead = kStages - 1;
+      constexpr std::integral_constant<int, TM + TN> reads{};
+      constexpr std::integral_constant<int, 0> none{};
+      multiply(std::integral_constant<int, 0>(), reads, std::integral_constant<int, (kAfter >= kAhead ? kCopies - kFirst : 0)>(), stage(block), block + kAhead, kFirst);
+      if constexpr (kSteps == 4) {
+        multiply(std::integral_constant<int, 1>(), reads, none, stage(block), 0, 0);
+        multiply(std::integral_constant<int, 2>(), reads, none, stage(block), 0, 0);
+      }
+      wait_vector_loads<(ASYNC && kAfter > 1 ? std::min(kAfter, kAhead) - 1 : 0) * kCopies>();
+      if constexpr (kAfter > 0) put(block + 1);
       lds_barrier();                                             // the next block is there, and nobody reads this one any more
-      multiply(std::integral_constant<int, 3>(), next_, after_, step + 1, step + 2);
+      multiply(std::integral_constant<int, kLast>(), std::integral_constant<int, (kAfter > 0 ? TM + TN : 0)>(), std::integral_constant<int, (kAfter > kAhead ? kFirst : 0)>(), stage(block + 1),
+               block + kStages, 0);
     };
-    if (own > 0) {
+    if constexpr (ASYNC) {
 #pragma unroll
-      for (int c = 0; c < kCopies; ++c) ask(0, c);
-      put(0);
-    }
-    if (own > 1) {
+      for (int b = 0; b < kStages - 1; ++b)
+        if (b < own)
 #pragma unroll
-      for (int c = 0; c < kFirst; ++c) ask(1, c);
-      if constexpr (ASYNC) wait_vector_loads<kFirst>();
+          for (int c = 0; c < kCopies; ++c) ask(b, stage(b), c);
+      if (kStages - 1 < own) {
+#pragma unroll
+        for (int c = 0; c < kFirst; ++c) ask(kStages - 1, stage(kStages - 1), c);
+        wait_vector_loads<(kStages - 2) * kCopies + kFirst>();
+      } else {
+        wait_all_vector_loads();
+      }
     } else {
-      wait_all_vector_loads();
+      if (own > 0) {
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) ask(0, nullptr, c);
+        put(0);
+      }
+      if (own > 1) {
+#pragma unroll
+        for (int c = 0; c < kFirst; ++c) ask(1, nullptr, c);
+      }
     }
     lds_barrier();
     if (own > 0) {
 #pragma unroll
-      for (int f = 0; f < TM + TN; ++f) read(0, 0, f);
+      for (int f = 0; f < TM + TN; ++f) read(stage(0), 0, f);
     }
-    int step = 0;
-    for (; step + 2 < own; ++step) block(step, Yes(), Yes());
-    if (step + 1 < own) block(step++, Yes(), No());
-    if (step < own) block(step++, No(), No());
-    for (; step < steps; ++step) lds_barrier();                  // (a team with a block less than the first)
-    if (whole < a.k_blocks()) {
+    int block = 0;
+    for (; block + kStages < own; ++block) multiply_block(block, std::integral_constant<int, kStages>());
+    if constexpr (ASYNC) {
+      if (block + 4 < own) multiply_block(block++, std::integral_constant<int, 4>());
+      if (block + 3 < own) multiply_block(block++, std::integral_constant<int, 3>());
+      if (block + 2 < own) multiply_block(block++, std::integral_constant<int, 2>());
+    }
+    if (block + 1 < own) multiply_block(block++, std::integral_constant<int, 1>());
+    if (block < own) multiply_block(block++, std::integral_constant<int, 0>());
+    for (; block < blocks; ++block) lds_barrier();               // (a team with a block less than the first)
+    if (whole * kBlock < a.k) {
       const bool mine = whole % KG == team;
       if (mine) put_end();                                       // (into a buffer that nobody reads since the last barrier)
       lds_barrier();
       if (mine) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < kSteps; ++q) {
 #pragma unroll
-          for (int f = 0; f < TM + TN; ++f) read(own, q, f);
+          for (int f = 0; f < TM + TN; ++f) read(stage(own), q, f);
 #pragma unroll
           for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] = product_32x32(wf[q & 1][i % TN], xf[q & 1][i / TN], acc[i / TN][i % TN]);
         }
@@ -397,50 +492,20 @@ __global__ __launch_bounds__(64 * WM * WN * KG, TM * TN >= 16 ? 1 : WM * WN * KG
     }
   }
   if (KG > 1 && team > 0) return;
-  int64_t from[TM];
-  float xs[TM];
-  bool fine = true;
-#pragma unroll
-  for (int m = 0; m < TM; ++m) {
-    const int64_t row = t.first + (wm * TM + m) * 32 + (lane & 31);
-    from[m] = t.group < 0 ? -1 : source_row<GROUPED>(a, min(row, t.end - 1));
-    xs[m] = from[m] >= 0 ? a.x_scales[from[m] * a.x_scales_stride] : 1.0f;
-    fine = fine && ordinary(xs[m]);
-  }
-#pragma unroll
-  for (int n = 0; n < TN; ++n) {
-    const int col = col0 + (wn * TN + n) * 32;
-    if (col >= a.n) break;
-    f32x4 ws[4];
-    bool ok = fine;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      ws[g] = weight_scales(a, max(t.group, 0), col + 8 * g + 4 * h);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) ok = ok && ordinary(ws[g][e]);
-    }
-    const bool exact = !__all(ok);
-#pragma unroll
-    for (int m = 0; m < TM; ++m) {
-      const int64_t row = t.first + (wm * TM + m) * 32 + (lane & 31);
-      f32x4 v[4];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        v[g] = scaled(i32x4{acc[m][n][4 * g], acc[m][n][4 * g + 1], acc[m][n][4 * g + 2], acc[m][n][4 * g + 3]}, xs[m], ws[g], exact);
-        if (from[m] < 0) v[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      }
-      switch (a.y_type) {
-        case LUTKAN_F32: store_32x32<LUTKAN_F32>(a, row, row < t.end, col, h, v); break;
-        case LUTKAN_F16: store_32x32<LUTKAN_F16>(a, row, row < t.end, col, h, v); break;
-        default: store_32x32<LUTKAN_BF16>(a, row, row < t.end, col, h, v); break;
-      }
-    }
+  if constexpr (KG == 1) lds_barrier();                          // nobody reads the buffers any more
+  unsigned char *const dump = s_tiles + T::kParts + wave * dump_bytes(TN);
+  const int64_t row0 = t.first + wm * TM * 32;
+  const int wave_col0 = col0 + wn * TN * 32;
+  switch (a.y_type) {
+    case LUTKAN_F32: store_wave<LUTKAN_F32, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump); break;
+    case LUTKAN_F16: store_wave<LUTKAN_F16, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump); break;
+    default: store_wave<LUTKAN_BF16, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump); break;
   }
 }
 
 template <int TM, int TN, int WM, int WN, int KG, bool GROUPED, bool ASYNC>
 int launch_tiles_as(ProductArgs a, int64_t row_tiles, const char *who, hipStream_t s) {
-  using T = Tile<TM, TN, WM, WN, KG>;
+  using T = Tile<TM, TN, WM, WN, KG, ASYNC>;
   static LdsCap cap;
   a.extent = (int32_t)row_tiles;
   const auto kernel = lutkan_int8_tiled_kernel<TM, TN, WM, WN, KG, GROUPED, ASYNC>;
