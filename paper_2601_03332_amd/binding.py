@@ -193,7 +193,8 @@ _native = None
 
 class _GeneralPath:
     """In place of the module where it cannot be loaded: every call takes the general path."""
-    lut_forward = lut_model_forward = spline_forward = rmsnorm_fp8 = quantise_fp8 = matmul_fp8 = staticmethod(lambda *args: None)
+    lut_forward = lut_model_forward = spline_forward = rmsnorm_fp8 = quantise_fp8 = matmul_fp8 = rmsnorm_int8 = quantise_int8 = matmul_int8 = \
+        expert_sort = expert_combine = expert_combine_backward = staticmethod(lambda *args: None)
 
 
 def _load_native():
@@ -205,8 +206,10 @@ def _load_native():
         spec.loader.exec_module(module)
         entries = (lib.lutkan_forward_or_workspace, lib.lutkan_forward, lib.lutkan_model_forward_or_workspace, lib.lutkan_model_forward,
                    lib.bspline_forward_workspace_bytes, lib.bspline_kan_forward, lib.lutkan_rmsnorm_fp8, lib.lutkan_quantise_fp8,
-                   lib.lutkan_matmul_fp8, lib.lutkan_grouped_matmul_fp8)
-        module.init(*[C.cast(f, C.c_void_p).value for f in entries], _DevLayer, _SplineDevLayer,
+                   lib.lutkan_matmul_fp8, lib.lutkan_grouped_matmul_fp8, lib.lutkan_rmsnorm_int8, lib.lutkan_quantise_int8, lib.lutkan_matmul_int8,
+                   lib.lutkan_grouped_matmul_int8, lib.lutkan_expert_sort_workspace_bytes, lib.lutkan_expert_sort, lib.lutkan_expert_combine,
+                   lib.lutkan_expert_combine_backward)
+        module.init(tuple(C.cast(f, C.c_void_p).value for f in entries), _DevLayer, _SplineDevLayer,
                     getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream))
         return module
     except Exception as error:
@@ -963,6 +966,10 @@ def lutkan_grouped_matmul_fp8(x, x_scales, weight, weight_scales, group_sizes, r
 def lutkan_rmsnorm_int8(x, weight, residual=None, eps: float = 1e-6, residual_out=None):
     """lutkan_rmsnorm_fp8 with integer codes and one scale a row: returns (codes, scales, residual_out), int8 [rows, width], float32 [rows], and
     x + residual in the residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself."""
+    if residual_out is None:
+        out = (_native or _native_calls()).rmsnorm_int8(x, weight, residual, eps)
+        if out is not None:
+            return out
     who, torch = "lutkan_rmsnorm_int8", _torch()
     _check_matrix(who, "x", x, (None, None), None)
     rows, width = x.shape
@@ -993,6 +1000,9 @@ def lutkan_rmsnorm_int8(x, weight, residual=None, eps: float = 1e-6, residual_ou
 def lutkan_quantise_int8(x):
     """(codes, scales) of a weight [n, k], of one weight per expert [experts, n, k], or of tokens [rows, k]: int8 of x's shape and a float32 scale
     for each row of it ([n], [experts, n], [rows]), for the products below."""
+    out = (_native or _native_calls()).quantise_int8(x)
+    if out is not None:
+        return out
     who, torch = "lutkan_quantise_int8", _torch()
     _check_matrix(who, "x", x, (None,) * (3 if isinstance(x, torch.Tensor) and x.dim() == 3 else 2), None)
     n, k = x.shape[-2:]
@@ -1038,6 +1048,10 @@ def lutkan_matmul_int8(x, x_scales, weight, weight_scales, y=None, dtype=None):
     is given (float32, which a layer takes, is the default; float16, bfloat16)."""
     who, torch = "lutkan_matmul_int8", _torch()
     dtype = torch.float32 if dtype is None else dtype
+    if y is None:
+        out = (_native or _native_calls()).matmul_int8(x, x_scales, weight, weight_scales, dtype)
+        if out is not None:
+            return out
     y, a = _matmul_int8(who, x, x_scales, weight, weight_scales, y, dtype, None, False)
     with torch.cuda.device(x.device):
         _check(load_library().lutkan_matmul_int8(C.byref(a), _stream(x.device)))
@@ -1061,6 +1075,10 @@ def lutkan_grouped_matmul_int8(x, x_scales, weight, weight_scales, group_sizes, 
     lutkan_expert_sort gives them."""
     who, torch = "lutkan_grouped_matmul_int8", _torch()
     dtype = torch.float32 if dtype is None else dtype
+    if y is None:
+        out = (_native or _native_calls()).matmul_int8(x, x_scales, weight, weight_scales, dtype, group_sizes, rows)
+        if out is not None:
+            return out
     _check_matrix(who, "x", x, (None, None), None, torch.int8)
     if rows is not None:
         _check_whole_numbers(who, "rows", rows, x.device)
@@ -1079,10 +1097,13 @@ def lutkan_grouped_matmul_int8(x, x_scales, weight, weight_scales, group_sizes, 
 # ---------------------------------------------------------------- a mixture of experts: choices sorted, rows joined (see lutkan.h)
 def lutkan_expert_sort(expert, experts: int):
     """A router's choices expert [tokens, top] (int32 or int64) sorted by expert, those of one expert in their order, on the current stream; nothing
-    waits for it.  Returns int32 tensors (rows, places, group_sizes):
+    waits for it.  Returns int32 tensors (rows, places, group_sizes), which are used together and may share one allocation:
         rows [tokens * top]   the token of each sorted row, -1 behind the last group (rows= of the grouped products)
         places [tokens, top]  the sorted row of each choice; -1 for a choice outside [0, experts), which belongs to no group
         group_sizes [experts]"""
+    out = (_native or _native_calls()).expert_sort(expert, experts)
+    if out is not None:
+        return out
     who, torch = "lutkan_expert_sort", _torch()
     if not isinstance(expert, torch.Tensor) or expert.dtype not in (torch.int32, torch.int64) or expert.dim() != 2 or not expert.is_cuda or expert.layout != torch.strided:
         raise LutKanError(f"{who}: expert must be an int32 or int64 CUDA tensor of shape [tokens, top]")
@@ -1117,6 +1138,10 @@ def lutkan_expert_combine(y, places, weights=None, out=None, dtype=None):
     lutkan_expert_sort gives them), weights [tokens, top] or None (1), on the current stream; summed in float32.  A place outside y adds nothing.
     dtype: of out where none is given (y's).  lutkan_expert_combine(x, rows[:, None]) brings tokens x into the experts' order, a row of zeros
     where rows is -1; the gradient of that is lutkan_expert_combine(gradient, places)."""
+    if out is None:
+        native = (_native or _native_calls()).expert_combine(y, places, weights, dtype)
+        if native is not None:
+            return native
     who, torch = "lutkan_expert_combine", _torch()
     _check_matrix(who, "y", y, (None, None), None)
     _check_whole_numbers(who, "places", places, y.device)
@@ -1147,6 +1172,9 @@ def lutkan_expert_combine_backward(grad, y, rows, places, weights=None):
     """The gradients of lutkan_expert_combine(y, places, weights) for the gradient grad [tokens, width] of its output: (grad_y [rows, width] in y's
     dtype, grad_weights [tokens, top] in the weights'; None without weights).  rows and places are of one lutkan_expert_sort; rows of grad_y that
     no place leads to are zeros.  The operators take no part in torch's autograd: a program calls this from its own backward pass."""
+    out = (_native or _native_calls()).expert_combine_backward(grad, y, rows, places, weights)
+    if out is not None:
+        return out
     who, torch = "lutkan_expert_combine_backward", _torch()
     _check_matrix(who, "grad", grad, (None, None), None)
     tokens, width = grad.shape

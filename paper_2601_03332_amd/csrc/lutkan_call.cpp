@@ -40,6 +40,14 @@ struct {
   decltype(&lutkan_quantise_fp8) quantise;
   decltype(&lutkan_matmul_fp8) matmul;
   decltype(&lutkan_grouped_matmul_fp8) grouped_matmul;
+  decltype(&lutkan_rmsnorm_int8) rmsnorm_int8;
+  decltype(&lutkan_quantise_int8) quantise_int8;
+  decltype(&lutkan_matmul_int8) matmul_int8;
+  decltype(&lutkan_grouped_matmul_int8) grouped_matmul_int8;
+  decltype(&lutkan_expert_sort_workspace_bytes) sort_workspace_bytes;
+  decltype(&lutkan_expert_sort) sort;
+  decltype(&lutkan_expert_combine) combine;
+  decltype(&lutkan_expert_combine_backward) combine_backward;
   PyObject *lut_struct, *spline_struct, *current_stream;
 } g;
 
@@ -228,11 +236,11 @@ bool on_device(const at::Tensor &x, const Work &work) {
   return work(stream) == LUTKAN_OK;
 }
 
-// A contiguous matrix in the memory of `held` (bytes), from byte `at` on.
-at::Tensor matrix_in(const at::Tensor &held, int64_t at, at::ScalarType type, int64_t rows, int64_t columns) {
+// A contiguous tensor in the memory of `held` (bytes), from byte `at` on.
+at::Tensor tensor_in(const at::Tensor &held, int64_t at, at::ScalarType type, at::IntArrayRef sizes) {
   at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(held.storage()), held.key_set(), c10::scalarTypeToTypeMeta(type));
   c10::TensorImpl *impl = t.unsafeGetTensorImpl();
-  impl->set_sizes_contiguous({rows, columns});
+  impl->set_sizes_contiguous(sizes);
   impl->set_storage_offset(at / (int64_t)c10::elementSize(type));
   return t;
 }
@@ -247,8 +255,18 @@ PyObject *wrapped(const at::Tensor &a, const at::Tensor &b) {
   return pair;
 }
 
-// rmsnorm_fp8(x, weight, residual or None, eps)
-PyObject *rmsnorm_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+PyObject *wrapped(const at::Tensor &a, const at::Tensor &b, PyObject *c) {                // (takes the reference to c)
+  PyObject *three = PyTuple_New(3), *x = THPVariable_Wrap(a), *y = THPVariable_Wrap(b);
+  if (!three || !x || !y || !c) { Py_XDECREF(three); Py_XDECREF(x); Py_XDECREF(y); Py_XDECREF(c); return nullptr; }
+  PyTuple_SET_ITEM(three, 0, x);
+  PyTuple_SET_ITEM(three, 1, y);
+  PyTuple_SET_ITEM(three, 2, c);
+  return three;
+}
+
+// rmsnorm_fp8(x, weight, residual or None, eps), and rmsnorm_int8
+template <bool INT8>
+PyObject *rmsnorm(PyObject *, PyObject *const *args, Py_ssize_t n) {
   try {
     if (n != 4 || !PyFloat_CheckExact(args[3])) return not_taken();
     const at::Tensor *x = plain_tensor(args[0]), *w = plain_tensor(args[1]), *r = args[2] == Py_None ? nullptr : plain_tensor(args[2]);
@@ -262,34 +280,31 @@ PyObject *rmsnorm_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const bool ok = on_device(*x, [&](void *stream) {
       const auto options = x->options().requires_grad(false);
       const int64_t scales_at = (rows * width + 255) / 256 * 256;            // codes and scales go together: one allocation, 0.5 us less
-      const at::Tensor held = at::empty({scales_at + rows * blocks(width) * 4}, options.dtype(at::kByte));
-      codes = matrix_in(held, 0, at::kFloat8_e4m3fn, rows, width);
-      scales = matrix_in(held, scales_at, at::kFloat, rows, blocks(width));
+      const int64_t scales_each = INT8 ? 1 : blocks(width);
+      const at::Tensor held = at::empty({scales_at + rows * scales_each * 4}, options.dtype(at::kByte));
+      codes = tensor_in(held, 0, INT8 ? at::kChar : at::kFloat8_e4m3fn, {rows, width});
+      scales = INT8 ? tensor_in(held, scales_at, at::kFloat, {rows}) : tensor_in(held, scales_at, at::kFloat, {rows, scales_each});
       a.x = x->const_data_ptr(); a.weight = w->const_data_ptr();
       a.codes = codes.mutable_data_ptr(); a.scales = scales.mutable_data_ptr<float>();
-      a.x_stride = row_stride(*x); a.codes_stride = width; a.scales_stride = blocks(width);
+      a.x_stride = row_stride(*x); a.codes_stride = width; a.scales_stride = scales_each;
       a.rows = rows; a.width = (int32_t)width; a.x_type = type_of(*x); a.weight_type = type_of(*w); a.eps = (float)PyFloat_AS_DOUBLE(args[3]);
       if (r) {
         out = at::empty({rows, width}, r->options().requires_grad(false));
         a.residual = r->const_data_ptr(); a.residual_type = type_of(*r); a.residual_stride = row_stride(*r);
         a.residual_out = out.mutable_data_ptr(); a.residual_out_stride = width;
       }
-      return g.rmsnorm(&a, stream);
+      return INT8 ? g.rmsnorm_int8(&a, stream) : g.rmsnorm(&a, stream);
     });
     if (!ok) return not_taken();
-    PyObject *three = PyTuple_New(3), *c = THPVariable_Wrap(codes), *s = THPVariable_Wrap(scales), *o = r ? THPVariable_Wrap(out) : none();
-    if (!three || !c || !s || !o) { Py_XDECREF(three); Py_XDECREF(c); Py_XDECREF(s); Py_XDECREF(o); return nullptr; }
-    PyTuple_SET_ITEM(three, 0, c);
-    PyTuple_SET_ITEM(three, 1, s);
-    PyTuple_SET_ITEM(three, 2, o);
-    return three;
+    return wrapped(codes, scales, r ? THPVariable_Wrap(out) : none());
   } catch (...) {
     return not_taken();
   }
 }
 
-// quantise_fp8(weight)
-PyObject *quantise_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// quantise_fp8(weight), and quantise_int8
+template <bool INT8>
+PyObject *quantise(PyObject *, PyObject *const *args, Py_ssize_t n) {
   try {
     const at::Tensor *w = n == 1 ? plain_tensor(args[0]) : nullptr;
     if (!w || intercepted() || type_of(*w) < 0 || !(is_rows(*w, 2) || is_rows(*w, 3))) return not_taken();
@@ -299,9 +314,16 @@ PyObject *quantise_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     at::Tensor codes, scales;
     const bool ok = on_device(*w, [&](void *stream) {
       const auto options = w->options().requires_grad(false);
-      codes = at::empty(w->sizes(), options.dtype(at::kFloat8_e4m3fn));
-      scales = several ? at::empty({w->size(0), blocks(rows), blocks(k)}, options.dtype(at::kFloat)) : at::empty({blocks(rows), blocks(k)}, options.dtype(at::kFloat));
-      return g.quantise(w->const_data_ptr(), type_of(*w), several ? w->size(0) : 1, (int32_t)rows, (int32_t)k, row_stride(*w), several ? w->stride(0) : 0,
+      if constexpr (INT8) {
+        const int64_t scales_at = (w->numel() + 255) / 256 * 256;
+        const at::Tensor held = at::empty({scales_at + (several ? w->size(0) : 1) * rows * 4}, options.dtype(at::kByte));
+        codes = tensor_in(held, 0, at::kChar, w->sizes());
+        scales = tensor_in(held, scales_at, at::kFloat, w->sizes().slice(0, w->dim() - 1));
+      } else {
+        codes = at::empty(w->sizes(), options.dtype(at::kFloat8_e4m3fn));
+        scales = several ? at::empty({w->size(0), blocks(rows), blocks(k)}, options.dtype(at::kFloat)) : at::empty({blocks(rows), blocks(k)}, options.dtype(at::kFloat));
+      }
+      return (INT8 ? g.quantise_int8 : g.quantise)(w->const_data_ptr(), type_of(*w), several ? w->size(0) : 1, (int32_t)rows, (int32_t)k, row_stride(*w), several ? w->stride(0) : 0,
                         codes.mutable_data_ptr(), scales.mutable_data_ptr<float>(), stream);
     });
     return ok ? wrapped(codes, scales) : not_taken();
@@ -312,8 +334,9 @@ PyObject *quantise_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 bool is_whole_numbers(const at::Tensor &t) { return t.dim() == 1 && t.is_contiguous() && (t.scalar_type() == at::kInt || t.scalar_type() == at::kLong); }
 
-// matmul_fp8(x, x_scales, weight, weight_scales, dtype) and, with two more, group_sizes and rows or None
-PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// matmul_fp8(x, x_scales, weight, weight_scales, dtype) and, with two more, group_sizes and rows or None; and matmul_int8
+template <bool INT8>
+PyObject *matmul(PyObject *, PyObject *const *args, Py_ssize_t n) {
   try {
     const bool grouped = n == 7;
     if ((n != 5 && n != 7) || !THPDtype_Check(args[4])) return not_taken();
@@ -321,10 +344,16 @@ PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor *sizes = grouped ? plain_tensor(args[5]) : nullptr, *index = grouped && args[6] != Py_None ? plain_tensor(args[6]) : nullptr;
     if (!x || !xs || !w || !ws || (grouped && (!sizes || (args[6] != Py_None && !index))) || intercepted()) return not_taken();
     const int64_t dims = grouped ? 3 : 2;
-    if (!is_rows(*x, 2) || !is_rows(*xs, 2) || !is_rows(*w, dims) || ws->dim() != dims || !ws->is_contiguous()) return not_taken();
-    if (x->scalar_type() != at::kFloat8_e4m3fn || w->scalar_type() != at::kFloat8_e4m3fn || xs->scalar_type() != at::kFloat || ws->scalar_type() != at::kFloat) return not_taken();
+    if (!is_rows(*x, 2) || !is_rows(*w, dims) || !ws->is_contiguous()) return not_taken();
+    constexpr at::ScalarType code = INT8 ? at::kChar : at::kFloat8_e4m3fn;
+    if (x->scalar_type() != code || w->scalar_type() != code || xs->scalar_type() != at::kFloat || ws->scalar_type() != at::kFloat) return not_taken();
     const int64_t k = x->size(1), columns = w->size(-2);
-    if (w->size(-1) != k || xs->size(0) != x->size(0) || xs->size(1) != blocks(k) || ws->size(-2) != blocks(columns) || ws->size(-1) != blocks(k)) return not_taken();
+    if (INT8) {
+      if (xs->dim() != 1 || ws->dim() != dims - 1 || ws->size(-1) != columns) return not_taken();
+    } else {
+      if (!is_rows(*xs, 2) || ws->dim() != dims || xs->size(1) != blocks(k) || ws->size(-2) != blocks(columns) || ws->size(-1) != blocks(k)) return not_taken();
+    }
+    if (w->size(-1) != k || xs->size(0) != x->size(0)) return not_taken();
     if (xs->device() != x->device() || w->device() != x->device() || ws->device() != x->device() || k > INT32_MAX || columns > INT32_MAX) return not_taken();
     if (grouped) {
       if (ws->size(0) != w->size(0) || w->size(0) > INT32_MAX || !is_whole_numbers(*sizes) || sizes->size(0) != w->size(0) || sizes->device() != x->device()) return not_taken();
@@ -337,7 +366,7 @@ PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
       y = at::empty({a.rows, columns}, x->options().requires_grad(false).dtype(reinterpret_cast<THPDtype *>(args[4])->scalar_type));
       a.x = x->const_data_ptr(); a.x_scales = xs->const_data_ptr<float>(); a.weight = w->const_data_ptr(); a.weight_scales = ws->const_data_ptr<float>();
       a.y = y.mutable_data_ptr();
-      a.x_rows = x->size(0); a.x_stride = row_stride(*x); a.x_scales_stride = row_stride(*xs); a.weight_stride = row_stride(*w); a.y_stride = columns;
+      a.x_rows = x->size(0); a.x_stride = row_stride(*x); a.x_scales_stride = INT8 ? xs->stride(0) : row_stride(*xs); a.weight_stride = row_stride(*w); a.y_stride = columns;
       a.weight_matrix_stride = grouped ? w->stride(0) : 0;
       a.k = (int32_t)k; a.n = (int32_t)columns; a.y_type = type_of(y);
       if (grouped) {
@@ -345,7 +374,7 @@ PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
         a.group_sizes = sizes->const_data_ptr(); a.group_sizes_bytes = (int32_t)sizes->element_size();
         if (index) { a.row_index = index->const_data_ptr(); a.row_index_bytes = (int32_t)index->element_size(); }
       }
-      return grouped ? g.grouped_matmul(&a, stream) : g.matmul(&a, stream);
+      return INT8 ? (grouped ? g.grouped_matmul_int8 : g.matmul_int8)(&a, stream) : (grouped ? g.grouped_matmul : g.matmul)(&a, stream);
     });
     return ok ? THPVariable_Wrap(y) : not_taken();
   } catch (...) {
@@ -353,21 +382,115 @@ PyObject *matmul_fp8(PyObject *, PyObject *const *args, Py_ssize_t n) {
   }
 }
 
-// init(addresses of the ten entry points, the two struct classes, the stream function)
+// expert_sort(expert, experts)
+PyObject *expert_sort(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  try {
+    const at::Tensor *e = n == 2 && PyLong_CheckExact(args[1]) ? plain_tensor(args[0]) : nullptr;
+    if (!e || intercepted() || !is_rows(*e, 2) || (e->scalar_type() != at::kInt && e->scalar_type() != at::kLong)) return not_taken();
+    const long experts = PyLong_AsLong(args[1]);
+    if (PyErr_Occurred() || experts < 1 || experts > LUTKAN_EXPERT_MAX) return not_taken();
+    const int64_t tokens = e->size(0), top = e->size(1);
+    if (top < 1 || tokens > LUTKAN_EXPERT_MAX_CHOICES / top) return not_taken();
+    at::Tensor rows, places, sizes;
+    const bool ok = on_device(*e, [&](void *stream) {
+      const size_t needed = g.sort_workspace_bytes(tokens, (int32_t)top, (int32_t)experts);
+      const int64_t each = (tokens * top * 4 + 255) / 256 * 256, sizes_at = 2 * each, workspace_at = sizes_at + (experts * 4 + 255) / 256 * 256;
+      const at::Tensor held = at::empty({workspace_at + (int64_t)needed}, e->options().requires_grad(false).dtype(at::kByte));      // one allocation for all
+      rows = tensor_in(held, 0, at::kInt, {tokens * top});
+      places = tensor_in(held, each, at::kInt, {tokens, top});
+      sizes = tensor_in(held, sizes_at, at::kInt, {experts});
+      lutkan_expert_sort_args a{};
+      a.expert = e->const_data_ptr(); a.rows = rows.mutable_data_ptr<int32_t>(); a.places = places.mutable_data_ptr<int32_t>(); a.group_sizes = sizes.mutable_data_ptr<int32_t>();
+      a.workspace = needed ? static_cast<char *>(held.mutable_data_ptr()) + workspace_at : nullptr; a.workspace_bytes = needed;
+      a.expert_stride = row_stride(*e); a.tokens = tokens; a.top = (int32_t)top; a.experts = (int32_t)experts; a.expert_bytes = (int32_t)e->element_size();
+      return g.sort(&a, stream);
+    });
+    return ok ? wrapped(rows, places, THPVariable_Wrap(sizes)) : not_taken();
+  } catch (...) {
+    return not_taken();
+  }
+}
+
+bool is_places(const at::Tensor *t, int64_t dims, c10::Device device) {
+  return t && t->dim() == dims && t->is_contiguous() && (t->scalar_type() == at::kInt || t->scalar_type() == at::kLong) && t->device() == device;
+}
+bool is_weights(const at::Tensor *w, const at::Tensor &places) {                   // (nullptr: none)
+  return !w || (w->dim() == 2 && w->size(0) == places.size(0) && w->size(1) == places.size(1) && w->is_contiguous() && type_of(*w) >= 0 && w->device() == places.device());
+}
+
+// expert_combine(y, places, weights or None, dtype or None)
+PyObject *expert_combine(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  try {
+    if (n != 4 || (args[3] != Py_None && !THPDtype_Check(args[3]))) return not_taken();
+    const at::Tensor *y = plain_tensor(args[0]), *places = plain_tensor(args[1]), *w = args[2] == Py_None ? nullptr : plain_tensor(args[2]);
+    if (!y || !places || (args[2] != Py_None && !w) || intercepted()) return not_taken();
+    if (!is_rows(*y, 2) || type_of(*y) < 0 || !is_places(places, 2, y->device()) || !is_weights(w, *places)) return not_taken();
+    if (y->size(1) > INT32_MAX || places->size(1) > INT32_MAX) return not_taken();
+    at::Tensor out;
+    const bool ok = on_device(*y, [&](void *stream) {
+      out = at::empty({places->size(0), y->size(1)}, args[3] == Py_None ? y->options().requires_grad(false) : y->options().requires_grad(false).dtype(reinterpret_cast<THPDtype *>(args[3])->scalar_type));
+      if (type_of(out) < 0) return (int)LUTKAN_EINVAL;
+      lutkan_expert_combine_args a{};
+      a.y = y->const_data_ptr(); a.places = places->const_data_ptr(); a.weights = w ? w->const_data_ptr() : nullptr; a.out = out.mutable_data_ptr();
+      a.y_rows = y->size(0); a.y_stride = row_stride(*y); a.out_stride = out.size(1); a.tokens = places->size(0);
+      a.top = (int32_t)places->size(1); a.width = (int32_t)y->size(1); a.y_type = type_of(*y); a.weights_type = w ? type_of(*w) : 0; a.out_type = type_of(out);
+      a.places_bytes = (int32_t)places->element_size();
+      return g.combine(&a, stream);
+    });
+    return ok ? THPVariable_Wrap(out) : not_taken();
+  } catch (...) {
+    return not_taken();
+  }
+}
+
+// expert_combine_backward(grad, y, rows, places, weights or None)
+PyObject *expert_combine_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  try {
+    if (n != 5) return not_taken();
+    const at::Tensor *grad = plain_tensor(args[0]), *y = plain_tensor(args[1]), *rows = plain_tensor(args[2]), *places = plain_tensor(args[3]);
+    const at::Tensor *w = args[4] == Py_None ? nullptr : plain_tensor(args[4]);
+    if (!grad || !y || !rows || !places || (args[4] != Py_None && !w) || intercepted()) return not_taken();
+    if (!is_rows(*grad, 2) || type_of(*grad) < 0 || !is_rows(*y, 2) || type_of(*y) < 0 || y->size(1) != grad->size(1) || y->device() != grad->device()) return not_taken();
+    if (!is_places(rows, 1, y->device()) || rows->size(0) != y->size(0) || !is_places(places, 2, y->device()) || places->size(0) != grad->size(0) || !is_weights(w, *places)) return not_taken();
+    if (y->size(1) > INT32_MAX || places->size(1) > INT32_MAX) return not_taken();
+    at::Tensor grad_y, grad_w;
+    const bool ok = on_device(*y, [&](void *stream) {
+      grad_y = at::empty({y->size(0), y->size(1)}, y->options().requires_grad(false));
+      lutkan_expert_combine_backward_args a{};
+      a.grad = grad->const_data_ptr(); a.rows = rows->const_data_ptr(); a.places = places->const_data_ptr(); a.grad_y = grad_y.mutable_data_ptr();
+      if (w) {
+        grad_w = at::empty({w->size(0), w->size(1)}, w->options().requires_grad(false));
+        a.y = y->const_data_ptr(); a.weights = w->const_data_ptr(); a.grad_weights = grad_w.mutable_data_ptr(); a.weights_type = type_of(*w);
+      }
+      a.y_rows = y->size(0); a.grad_stride = row_stride(*grad); a.y_stride = row_stride(*y); a.grad_y_stride = y->size(1); a.tokens = grad->size(0);
+      a.top = (int32_t)places->size(1); a.width = (int32_t)y->size(1); a.grad_type = type_of(*grad); a.y_type = type_of(*y);
+      a.rows_bytes = (int32_t)rows->element_size(); a.places_bytes = (int32_t)places->element_size();
+      return g.combine_backward(&a, stream);
+    });
+    if (!ok) return not_taken();
+    PyObject *pair = PyTuple_New(2), *gy = THPVariable_Wrap(grad_y), *gw = w ? THPVariable_Wrap(grad_w) : none();
+    if (!pair || !gy || !gw) { Py_XDECREF(pair); Py_XDECREF(gy); Py_XDECREF(gw); return nullptr; }
+    PyTuple_SET_ITEM(pair, 0, gy);
+    PyTuple_SET_ITEM(pair, 1, gw);
+    return pair;
+  } catch (...) {
+    return not_taken();
+  }
+}
+
+// init(a tuple of the entry points' addresses, in the order of g's members, the two struct classes, the stream function)
 PyObject *init(PyObject *, PyObject *args) {
-  unsigned long long p[10];
-  PyObject *lut_struct, *spline_struct, *current_stream;
-  if (!PyArg_ParseTuple(args, "KKKKKKKKKKOOO", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &lut_struct, &spline_struct, &current_stream)) return nullptr;
-  g.forward_or_workspace = reinterpret_cast<decltype(g.forward_or_workspace)>(p[0]);
-  g.forward = reinterpret_cast<decltype(g.forward)>(p[1]);
-  g.model_or_workspace = reinterpret_cast<decltype(g.model_or_workspace)>(p[2]);
-  g.model = reinterpret_cast<decltype(g.model)>(p[3]);
-  g.spline_workspace_bytes = reinterpret_cast<decltype(g.spline_workspace_bytes)>(p[4]);
-  g.spline = reinterpret_cast<decltype(g.spline)>(p[5]);
-  g.rmsnorm = reinterpret_cast<decltype(g.rmsnorm)>(p[6]);
-  g.quantise = reinterpret_cast<decltype(g.quantise)>(p[7]);
-  g.matmul = reinterpret_cast<decltype(g.matmul)>(p[8]);
-  g.grouped_matmul = reinterpret_cast<decltype(g.grouped_matmul)>(p[9]);
+  constexpr int kEntries = 18;
+  PyObject *entries, *lut_struct, *spline_struct, *current_stream;
+  if (!PyArg_ParseTuple(args, "O!OOO", &PyTuple_Type, &entries, &lut_struct, &spline_struct, &current_stream)) return nullptr;
+  if (PyTuple_GET_SIZE(entries) != kEntries) return PyErr_Format(PyExc_TypeError, "%d entry points", kEntries);
+  int at = 0;
+  const auto take = [&](auto *to) { *to = reinterpret_cast<std::remove_pointer_t<decltype(to)>>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(entries, at++))); };
+  take(&g.forward_or_workspace); take(&g.forward); take(&g.model_or_workspace); take(&g.model); take(&g.spline_workspace_bytes); take(&g.spline);
+  take(&g.rmsnorm); take(&g.quantise); take(&g.matmul); take(&g.grouped_matmul);
+  take(&g.rmsnorm_int8); take(&g.quantise_int8); take(&g.matmul_int8); take(&g.grouped_matmul_int8);
+  take(&g.sort_workspace_bytes); take(&g.sort); take(&g.combine); take(&g.combine_backward);
+  if (PyErr_Occurred()) return nullptr;
   Py_INCREF(lut_struct); Py_INCREF(spline_struct); Py_INCREF(current_stream);
   g.lut_struct = lut_struct; g.spline_struct = spline_struct; g.current_stream = current_stream;
   Py_RETURN_NONE;
@@ -377,9 +500,15 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          {"lut_forward", (PyCFunction)(void (*)())lut_forward, METH_FASTCALL, nullptr},
                          {"lut_model_forward", (PyCFunction)(void (*)())lut_model_forward, METH_FASTCALL, nullptr},
                          {"spline_forward", (PyCFunction)(void (*)())spline_forward, METH_FASTCALL, nullptr},
-                         {"rmsnorm_fp8", (PyCFunction)(void (*)())rmsnorm_fp8, METH_FASTCALL, nullptr},
-                         {"quantise_fp8", (PyCFunction)(void (*)())quantise_fp8, METH_FASTCALL, nullptr},
-                         {"matmul_fp8", (PyCFunction)(void (*)())matmul_fp8, METH_FASTCALL, nullptr},
+                         {"rmsnorm_fp8", (PyCFunction)(void (*)())rmsnorm<false>, METH_FASTCALL, nullptr},
+                         {"quantise_fp8", (PyCFunction)(void (*)())quantise<false>, METH_FASTCALL, nullptr},
+                         {"matmul_fp8", (PyCFunction)(void (*)())matmul<false>, METH_FASTCALL, nullptr},
+                         {"rmsnorm_int8", (PyCFunction)(void (*)())rmsnorm<true>, METH_FASTCALL, nullptr},
+                         {"quantise_int8", (PyCFunction)(void (*)())quantise<true>, METH_FASTCALL, nullptr},
+                         {"matmul_int8", (PyCFunction)(void (*)())matmul<true>, METH_FASTCALL, nullptr},
+                         {"expert_sort", (PyCFunction)(void (*)())expert_sort, METH_FASTCALL, nullptr},
+                         {"expert_combine", (PyCFunction)(void (*)())expert_combine, METH_FASTCALL, nullptr},
+                         {"expert_combine_backward", (PyCFunction)(void (*)())expert_combine_backward, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lutkan_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -274,14 +274,15 @@ __device__ __forceinline__ void wait_vector_loads() { __builtin_amdgcn_s_waitcnt
 template <int TM, int TN, int WM, int WN, int KG, bool ASYNC>
 struct Tile {
   static constexpr int kRows = 32 * TM * WM, kCols = 32 * TN * WN, kThreads = 64 * WM * WN;
-  static constexpr int kBlock = ASYNC ? 64 : 128, kStages = ASYNC ? 5 : 2, kStage = (kRows + kCols) * kBlock;
+  static constexpr int kBlock = ASYNC ? 64 : 128, kStage = (kRows + kCols) * kBlock, kHalf = lutkan::kLdsPerWorkGroup / 2;
+  static constexpr int kStages = !ASYNC ? 2 : KG * 5 * kStage <= kHalf || WM * WN * KG > 4 ? 5 : kHalf / kStage;
   static constexpr int kParts = KG > 1 ? (KG - 1) * kRows * kCols * 4 : 0;       // the sums of all teams but the one that adds them up
   static constexpr int kLds = std::max(KG * kStages * kStage, kParts + WM * WN * dump_bytes(TN));
   static_assert(kLds <= lutkan::kLdsPerWorkGroup, "LDS");
 };
 
 template <int TM, int TN, int WM, int WN, int KG, bool GROUPED, bool ASYNC>
-__global__ __launch_bounds__(64 * WM * WN * KG, TM * TN >= 16 ? 1 : WM * WN * KG >= 16 ? 4 : 2) void lutkan_int8_tiled_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void lutkan_int8_tiled_kernel(const ProductArgs a) {
   using T = Tile<TM, TN, WM, WN, KG, ASYNC>;
   constexpr int kRows = T::kRows, kCols = T::kCols, kWaves = WM * WN, kBlock = T::kBlock, kStages = T::kStages, kStage = T::kStage, kSteps = kBlock / 32, kPieces = kBlock / 16;
   constexpr int kCopyRows = 1024 / kBlock, kXCopies = kRows / kCopyRows / kWaves, kWCopies = kCols / kCopyRows / kWaves, kCopies = kXCopies + kWCopies;     // for each wave
@@ -442,9 +443,13 @@ __global__ __launch_bounds__(64 * WM * WN * KG, TM * TN >= 16 ? 1 : WM * WN * KG
     }
     int block = 0;
     for (; block + kStages < own; ++block) multiply_block(block, std::integral_constant<int, kStages>());
-    if constexpr (ASYNC) {
+    if constexpr (kStages > 4) {
       if (block + 4 < own) multiply_block(block++, std::integral_constant<int, 4>());
+    }
+    if constexpr (kStages > 3) {
       if (block + 3 < own) multiply_block(block++, std::integral_constant<int, 3>());
+    }
+    if constexpr (kStages > 2) {
       if (block + 2 < own) multiply_block(block++, std::integral_constant<int, 2>());
     }
     if (block + 1 < own) multiply_block(block++, std::integral_constant<int, 1>());
@@ -549,7 +554,7 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
     const double step = async ? 1 : side == 64 ? 1.75 : 1.5;     // (through registers a step waits longer)
     return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one * step, all * step, ends + end_block, std::ceil(a.k / kScaleBlock / (double)teams), GROUPED);
   };
-  enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kKernels };
+  enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kTiled128x256, kKernels };
   double price[kKernels];
   price[kDirect16x16] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 16, a);
   price[kDirect16x32] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 32, a);
@@ -560,6 +565,7 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   price[kTiled128x2] = tiled(128, 1, 1.0, 1.0, 5, 2);
   price[kTiled128] = tiled(128, 2, 0.65, 1.08, 2, 1);
   price[kTiled256] = tiled(256, 1, 1.3, 1.3, 6, 1);
+  price[kTiled128x256] = async ? 1e300 : HUGE_VAL;
   if (GROUPED)                                                   // (weights that few rows share come from memory)
     for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.7;
   if (!aligned)                                                  // (five dwords for every four)
@@ -572,7 +578,8 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
   if (beyond_a_launch(64, 512)) price[kTiled64x2] = HUGE_VAL;
   if (beyond_a_launch(128, 512)) price[kTiled128x2] = HUGE_VAL;
   if (beyond_a_launch(128, 256)) price[kTiled128] = HUGE_VAL;
-  if (beyond_a_launch(256, 256)) price[kTiled256] = HUGE_VAL;
+  if (beyond_a_launch(256, 512)) price[kTiled256] = HUGE_VAL;
+  if (!lutkan::launch_holds(tiles(128) * ((a.n + 255) / 256), 256)) price[kTiled128x256] = HUGE_VAL;
   const int pick = (int)(std::min_element(price, price + kKernels) - price);
   if (price[pick] == HUGE_VAL) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   switch (pick) {
@@ -582,7 +589,8 @@ int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
     case kTiled64x4: return launch_tiles<1, 1, 2, 2, 4, GROUPED>(a, tiles(64), async, who, s);
     case kTiled64x2: return launch_tiles<1, 1, 2, 2, 2, GROUPED>(a, tiles(64), async, who, s);
     case kTiled128x2: return launch_tiles<2, 2, 2, 2, 2, GROUPED>(a, tiles(128), async, who, s);
-    case kTiled256: return launch_tiles_as<4, 4, 2, 2, 1, GROUPED, true>(a, tiles(256), who, s);
+    case kTiled128x256: return launch_tiles_as<2, 4, 2, 2, 1, GROUPED, true>(a, tiles(128), who, s);
+    case kTiled256: return launch_tiles_as<4, 2, 2, 4, 1, GROUPED, true>(a, tiles(256), who, s);
     default: return launch_tiles<2, 2, 2, 2, 1, GROUPED>(a, tiles(128), async, who, s);
   }
 }
