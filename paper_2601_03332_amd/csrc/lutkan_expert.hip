@@ -25,13 +25,14 @@ struct SortArgs {
 static_assert(sizeof(SortArgs) <= 112, "launch");
 
 constexpr int kSortWaves = 16;
-constexpr int kSortSingle = 16384;                                // choices of one work-group's launch
+constexpr int kSortHeld = 16;                                     // chunks of 64 choices whose experts a wave holds
+constexpr int kSortSingle = 64 * kSortHeld * kSortWaves;          // choices of one work-group's launch
 constexpr int kSortDigit = 11, kSortBins = (1 << kSortDigit) + 1; // (2048 experts and the dropped ones)
 
 // The expert of choice c, `experts` for a choice that is dropped.
 __device__ __forceinline__ int expert_of(const SortArgs &a, int c) {
-  const int token = c / a.top;
-  const int64_t e = whole_number(a.expert, token * a.stride + (c - token * a.top), a.expert_bytes);
+  const int64_t at = a.stride == a.top ? c : c / a.top * a.stride + c % a.top;
+  const int64_t e = whole_number(a.expert, at, a.expert_bytes);
   return e >= 0 && e < a.experts ? (int)e : a.experts;
 }
 // (One pass: all bits.)
@@ -47,11 +48,35 @@ __device__ __forceinline__ unsigned long long same_bin(int bin, int bits, bool h
   return same;
 }
 
-// How many choices of each bin the work-group's waves hold: s_count [wave][bins].
-__device__ __forceinline__ void count_bins(const SortArgs &a, int *s_count, int first, int last, int wave, int waves) {
+// A wave's choices of kSortHeld chunks of 64: which ones, and their experts, all asked for at once.
+struct SortHeld {
+  int choice[kSortHeld], expert[kSortHeld];
+  __device__ __forceinline__ void read(const SortArgs &a, int first, int last) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < kSortHeld; ++k) {
+      const int i = first + 64 * k + lane;
+      choice[k] = a.order && i < last ? a.order[i] : i;
+    }
+#pragma unroll
+    for (int k = 0; k < kSortHeld; ++k) {
+      const int i = first + 64 * k + lane;
+      expert[k] = i < last ? expert_of(a, choice[k]) : 0;
+    }
+  }
+};
+
+// How many choices of each bin the work-group's waves hold: s_count [wave][bins].  `held` keeps the last chunks.
+__device__ __forceinline__ void count_bins(const SortArgs &a, int *s_count, SortHeld &held, int first, int last, int wave, int waves) {
+  held.read(a, first, last);
   for (int i = threadIdx.x; i < waves * a.bins; i += blockDim.x) s_count[i] = 0;
   __syncthreads();
-  for (int i = first + (threadIdx.x & 63); i < last; i += 64) atomicAdd(&s_count[wave * a.bins + bin_of(a, expert_of(a, a.order ? a.order[i] : i))], 1);
+  for (int at = first; at < last; at += 64 * kSortHeld) {
+    if (at != first) held.read(a, at, last);
+#pragma unroll
+    for (int k = 0; k < kSortHeld; ++k)
+      if (at + 64 * k + (int)(threadIdx.x & 63) < last) atomicAdd(&s_count[wave * a.bins + bin_of(a, held.expert[k])], 1);
+  }
   __syncthreads();
 }
 
@@ -59,7 +84,8 @@ __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_count_kernel(co
   extern __shared__ int s_count[];
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int64_t first = ((int64_t)blockIdx.x * waves + wave) * a.segment;
-  count_bins(a, s_count, (int)min(first, (int64_t)a.choices), (int)min(first + a.segment, (int64_t)a.choices), wave, waves);
+  SortHeld held;
+  count_bins(a, s_count, held, (int)min(first, (int64_t)a.choices), (int)min(first + a.segment, (int64_t)a.choices), wave, waves);
   for (int e = threadIdx.x; e < a.bins; e += blockDim.x) {
     int sum = 0;
     for (int w = 0; w < waves; ++w) sum += s_count[w * a.bins + e];
@@ -68,31 +94,43 @@ __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_count_kernel(co
 }
 
 // A counting sort: the place of a choice is the number of choices of lower bins, of its bin in work-groups and waves before its own, and before it
-// in its wave.  The last comes from ballots over the bits of the bin, so that equal bins keep their order and no atomic decides it.
+// in its wave.  The last comes from ballots over the bits of the bin, so that equal bins keep their order and no atomic decides it (the atomics
+// here count).  Bound by latencies: launches, a chain of loads, counts and scans.
 template <bool SEVERAL>
 __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_sort_kernel(const SortArgs a) {
-  extern __shared__ int s_count[];                                // [waves][bins], then the bins' first places and totals, then the waves' sums
+  extern __shared__ int s_count[];                                // [waves][bins], then the bins' totals, later first places, the waves' sums, the bins' counts before
   const int bins = a.bins, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  int *s_total = s_count + waves * bins, *s_wave = s_total + bins;
+  int *s_total = s_count + waves * bins, *s_wave = s_total + bins, *s_before = s_wave + kSortWaves;
   const int64_t begin = ((int64_t)blockIdx.x * waves + wave) * a.segment;
   const int first = (int)min(begin, (int64_t)a.choices), last = (int)min(begin + a.segment, (int64_t)a.choices);
-  count_bins(a, s_count, first, last, wave, waves);
-  // Every bin: its total and, in place of the waves' counts, how many of it lie before each wave.
-  for (int e = threadIdx.x; e < bins; e += blockDim.x) {
-    int before = 0, total = 0;
-    if constexpr (SEVERAL) {
-      for (unsigned g = 0; g < gridDim.x; ++g) {
+  if constexpr (SEVERAL)
+    for (int e = threadIdx.x; e < bins; e += blockDim.x) s_total[e] = s_before[e] = 0;
+  SortHeld held;
+  count_bins(a, s_count, held, first, last, wave, waves);
+  if constexpr (SEVERAL) {                                        // the work-groups' counts: as many threads to a bin as there are
+    const int parts = max(1, (int)blockDim.x / bins), part = threadIdx.x / bins;
+    for (int e = parts > 1 ? threadIdx.x % bins : threadIdx.x; e < bins && part < parts; e += parts > 1 ? bins : blockDim.x) {
+      int before = 0, total = 0;
+#pragma unroll 8
+      for (int g = parts > 1 ? part : 0; g < (int)gridDim.x; g += parts) {
         const int n = a.counts[(int64_t)g * bins + e];
-        before += g < blockIdx.x ? n : 0;
+        before += g < (int)blockIdx.x ? n : 0;
         total += n;
       }
+      atomicAdd(&s_before[e], before);
+      atomicAdd(&s_total[e], total);
     }
+    __syncthreads();
+  }
+  // Every bin: in place of the waves' counts, how many of it lie before each wave.
+  for (int e = threadIdx.x; e < bins; e += blockDim.x) {
+    int before = SEVERAL ? s_before[e] : 0;
     for (int w = 0; w < waves; ++w) {
       const int n = s_count[w * bins + e];
       s_count[w * bins + e] = before;
       before += n;
     }
-    s_total[e] = SEVERAL ? total : before;
+    if constexpr (!SEVERAL) s_total[e] = before;
   }
   __syncthreads();
   // The bins' first places: sums of runs of bins, a run to a thread, then the run itself.
@@ -117,25 +155,30 @@ __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_sort_kernel(con
   }
   __syncthreads();
   const int bits = 32 - __builtin_clz(bins - 1);                  // (bins >= 2)
-  for (int i0 = first; i0 < last; i0 += 64) {
-    const int i = i0 + lane;
-    const bool here = i < last;
-    const int c = !here ? 0 : a.order ? a.order[i] : i, expert = here ? expert_of(a, c) : 0, bin = bin_of(a, expert);
-    const unsigned long long same = same_bin(bin, bits, here);
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    if (here) {
-      const int place = s_total[bin] + s_count[wave * bins + bin] + rank;
-      const bool held = expert < a.experts;
-      if (a.rows) {
-        a.rows[place] = held ? c / a.top : -1;
-        a.places[c] = held ? place : -1;
+  const bool again = last - first > 64 * kSortHeld;               // (the chunks that are held are the last)
+  for (int i0 = first; i0 < last; i0 += 64 * kSortHeld) {
+    if (again) held.read(a, i0, last);
+#pragma unroll
+    for (int k = 0; k < kSortHeld; ++k) {
+      if (i0 + 64 * k >= last) break;
+      const bool here = i0 + 64 * k + lane < last;
+      const int c = held.choice[k], expert = held.expert[k], bin = bin_of(a, expert);
+      const unsigned long long same = same_bin(bin, bits, here);
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      if (here) {
+        const int place = s_total[bin] + s_count[wave * bins + bin] + rank;
+        const bool is_held = expert < a.experts;
+        if (a.rows) {
+          a.rows[place] = is_held ? c / a.top : -1;
+          a.places[c] = is_held ? place : -1;
+        }
+        if (a.order_out) a.order_out[place] = c;
+        if (a.sorted) a.sorted[place] = expert;
       }
-      if (a.order_out) a.order_out[place] = c;
-      if (a.sorted) a.sorted[place] = expert;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // all lanes have read the count before its first lane raises it
+      if (here && rank == 0) s_count[wave * bins + bin] += __popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // all lanes have read the count before its first lane raises it
-    if (here && rank == 0) s_count[wave * bins + bin] += __popcll(same);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
@@ -168,7 +211,7 @@ SortPlan plan_sort(int64_t choices, int experts) {
     p.segment = (int)((chunks + p.waves - 1) / p.waves * 64);
     p.groups = 1;
   } else {
-    const int64_t of_wave = std::max<int64_t>(4, (chunks + 256 * kSortWaves - 1) / (256 * kSortWaves));
+    const int64_t of_wave = std::max<int64_t>(2, (chunks + 256 * kSortWaves - 1) / (256 * kSortWaves));
     p.waves = kSortWaves;
     p.segment = (int)(of_wave * 64);
     p.groups = (int)((chunks + of_wave * kSortWaves - 1) / (of_wave * kSortWaves));
@@ -182,7 +225,7 @@ SortPlan plan_sort(int64_t choices, int experts) {
 
 int launch_sort(const SortArgs &a, const SortPlan &p, const char *who, hipStream_t s) {
   static LdsCap caps[3];
-  const size_t counts = (size_t)p.waves * p.bins * sizeof(int), lds = counts + ((size_t)p.bins + kSortWaves) * sizeof(int);
+  const size_t counts = (size_t)p.waves * p.bins * sizeof(int), lds = counts + ((size_t)p.bins * (p.groups > 1 ? 2 : 1) + kSortWaves) * sizeof(int);
   lutkan::plan_note("expert_sort groups=%d waves=%d; ", p.groups, p.waves);
   if (p.groups == 1) {
     if (int rc = raise_lds_cap(lutkan_expert_sort_kernel<false>, &caps[0], who)) return rc;
@@ -232,6 +275,39 @@ __device__ __forceinline__ void write8(unsigned char *row, int col, int width, c
   for (int e = 0; e < 8; ++e) if (col + e < width) store_one<TYPE>(row + (size_t)(col + e) * type_bytes(TYPE), v[e]);
 }
 
+// Eight columns as they lie in memory, asked for and used later; a row that ends inside them is read element by element.
+template <int TYPE>
+struct Asked8 {
+  Raw8<TYPE> raw;
+  __device__ __forceinline__ void ask(const unsigned char *row, int col, int width) {
+    if (col + 8 <= width) raw = load_raw8<TYPE>(row + (size_t)col * type_bytes(TYPE));
+  }
+  __device__ __forceinline__ void get(const unsigned char *row, int col, int width, float (&v)[8]) const {
+    if (col + 8 <= width) values8<TYPE>(raw, v);
+    else read8<TYPE>(row, col, width, v);
+  }
+};
+
+// Up to 64 of a token's choices, one a lane: their rows of y (-1: none) and weights.
+struct Choices {
+  int row;
+  float weight;
+  __device__ __forceinline__ Choices(const void *places, int places_bytes, const unsigned char *weights, int weights_type, int64_t token, int top, int first, int64_t y_rows) {
+    const int j = first + (int)(threadIdx.x & 63);
+    row = -1;
+    weight = 1.0f;
+    if (j < top) {
+      const int64_t place = whole_number(places, token * top + j, places_bytes);
+      if (place >= 0 && place < y_rows) row = (int)place;
+      if (weights) weight = weight_at(weights, weights_type, token * top + j);
+    }
+  }
+  __device__ __forceinline__ int row_of(int j) const { return __builtin_amdgcn_readlane(row, j); }
+  __device__ __forceinline__ float weight_of(int j) const { return __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(weight), j)); }
+};
+
+constexpr int kJoined = 4;                                       // rows that are read before the first is used
+
 // A wave sums 512 columns of one token, eight a lane.
 template <int Y, int O>
 __global__ __launch_bounds__(256) void lutkan_expert_combine_kernel(const CombineArgs a) {
@@ -240,14 +316,27 @@ __global__ __launch_bounds__(256) void lutkan_expert_combine_kernel(const Combin
   if (token >= a.tokens) return;
   const int col = (int)(unit - token * pieces) * 512 + 8 * lane;
   float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  for (int j = 0; j < a.top; ++j) {
-    const int64_t place = whole_number(a.places, token * a.top + j, a.places_bytes);
-    if (place < 0 || place >= a.y_rows || col >= a.width) continue;
-    float v[8];
-    read8<Y>(a.y + place * a.y_stride * type_bytes(Y), col, a.width, v);
-    const float w = a.weights ? weight_at(a.weights, a.weights_type, token * a.top + j) : 1.0f;
+  for (int first = 0; first < a.top; first += 64) {
+    const Choices choices(a.places, a.places_bytes, a.weights, a.weights_type, token, a.top, first, a.y_rows);
+    const int count = min(a.top - first, 64);
+    for (int j0 = 0; j0 < count; j0 += kJoined) {
+      Asked8<Y> asked[kJoined];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += w * v[e];             // (two roundings, as an elementwise product and a sum have)
+      for (int j = 0; j < kJoined; ++j) {                        // (lanes behind the last choice hold none)
+        const int row = j0 + j < 64 ? choices.row_of(j0 + j) : -1;
+        if (row >= 0) asked[j].ask(a.y + row * a.y_stride * type_bytes(Y), col, a.width);
+      }
+#pragma unroll
+      for (int j = 0; j < kJoined; ++j) {
+        const int row = j0 + j < 64 ? choices.row_of(j0 + j) : -1;
+        if (row < 0) continue;
+        float v[8];
+        asked[j].get(a.y + row * a.y_stride * type_bytes(Y), col, a.width, v);
+        const float w = choices.weight_of(j0 + j);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += w * v[e];          // (two roundings, as an elementwise product and a sum have)
+      }
+    }
   }
   if (col < a.width) write8<O>(a.out + token * a.out_stride * type_bytes(O), col, a.width, sum);
 }
@@ -256,21 +345,21 @@ struct BackwardArgs {
   const unsigned char *grad, *y, *weights;
   const void *rows, *places;
   unsigned char *grad_y, *grad_weights;
-  int64_t y_rows, tokens;
+  int32_t y_rows, tokens;
   int32_t grad_stride, y_stride, grad_y_stride;
-  int32_t top, width;
+  int32_t top, width, checks;                                    // checks: work-groups that look for rows without a choice
   int8_t weights_type, rows_bytes, places_bytes;
 };
 static_assert(sizeof(BackwardArgs) <= 112, "launch");
 
-// A work-group takes a token: its waves share the columns, and their sums meet in LDS in the waves' order.  Work-groups behind the last token's look through the rows of y
-// for those that no place leads to, 64 each.
+// A work-group takes a token: its waves share the columns, and their sums meet in LDS in the waves' order.  The first work-groups look through the rows
+// of y for those that no place leads to, 64 each.
 template <int G, int Y>
 __global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(const BackwardArgs a) {
-  __shared__ float s_sum[16];
+  __shared__ float s_sum[16][kJoined];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  if (blockIdx.x >= a.tokens) {
-    const int64_t row = ((int64_t)blockIdx.x - a.tokens) * 64 + lane;
+  if ((int)blockIdx.x < a.checks) {
+    const int64_t row = (int64_t)blockIdx.x * 64 + lane;
     bool found = row >= a.y_rows;
     if (!found) {
       const int64_t token = whole_number(a.rows, row, a.rows_bytes);
@@ -284,36 +373,67 @@ __global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(co
     }
     return;
   }
-  const int64_t token = blockIdx.x;
+  const int64_t token = blockIdx.x - a.checks;
   const unsigned char *grad = a.grad + token * a.grad_stride * type_bytes(G);
-  for (int j = 0; j < a.top; ++j) {
-    const int64_t place = whole_number(a.places, token * a.top + j, a.places_bytes);
-    const bool held = place >= 0 && place < a.y_rows && whole_number(a.rows, place, a.rows_bytes) == token;      // (the work-group's: token, j)
-    const float w = held && a.weights ? weight_at(a.weights, a.weights_type, token * a.top + j) : 1.0f;
-    float dot = 0.0f;
-    for (int col = 8 * (int)threadIdx.x; held && col < a.width; col += 8 * blockDim.x) {
-      float g[8], v[8];
-      read8<G>(grad, col, a.width, g);
-      if (a.weights) {
-        read8<Y>(a.y + place * a.y_stride * type_bytes(Y), col, a.width, v);
+  for (int first = 0; first < a.top; first += 64) {
+    const Choices choices(a.places, a.places_bytes, a.weights, a.weights_type, token, a.top, first, a.y_rows);
+    const unsigned long long held = __ballot(choices.row >= 0 && whole_number(a.rows, choices.row, a.rows_bytes) == token);      // (one way and back)
+    const int count = min(a.top - first, 64);
+    for (int j0 = 0; j0 < count; j0 += kJoined) {
+      float dot[kJoined];
+      int row[kJoined];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dot = fmaf(g[e], v[e], dot);
+      for (int j = 0; j < kJoined; ++j) {
+        dot[j] = 0.0f;
+        row[j] = j0 + j < 64 && (held >> ((j0 + j) & 63) & 1) ? choices.row_of(j0 + j) : -1;
       }
+      for (int col = 8 * (int)threadIdx.x; col < a.width; col += 8 * blockDim.x) {
+        Asked8<G> asked;
+        Asked8<Y> of_y[kJoined];
+        asked.ask(grad, col, a.width);
+        if (a.weights)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] *= w;
-      write8<Y>(a.grad_y + place * a.grad_y_stride * type_bytes(Y), col, a.width, g);
-    }
-    if (!a.weights) continue;
+          for (int j = 0; j < kJoined; ++j) if (row[j] >= 0) of_y[j].ask(a.y + row[j] * (int64_t)a.y_stride * type_bytes(Y), col, a.width);
+        float g[8];
+        asked.get(grad, col, a.width, g);
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off);
-    if (waves > 1) {
-      if (lane == 0) s_sum[wave] = dot;
-      __syncthreads();
-      dot = 0.0f;
-      for (int o = 0; o < waves; ++o) dot += s_sum[o];
-      __syncthreads();
+        for (int j = 0; j < kJoined; ++j) {
+          if (row[j] < 0) continue;
+          float v[8];
+          if (a.weights) {
+            of_y[j].get(a.y + row[j] * (int64_t)a.y_stride * type_bytes(Y), col, a.width, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot[j] = fmaf(g[e], v[e], dot[j]);
+          }
+          const float w = choices.weight_of(j0 + j);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = g[e] * w;
+          write8<Y>(a.grad_y + row[j] * (int64_t)a.grad_y_stride * type_bytes(Y), col, a.width, v);
+        }
+      }
+      if (!a.weights) continue;
+#pragma unroll
+      for (int j = 0; j < kJoined; ++j)
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) dot[j] += __shfl_xor(dot[j], off);
+      if (waves > 1) {
+        if (lane == 0)
+#pragma unroll
+          for (int j = 0; j < kJoined; ++j) s_sum[wave][j] = dot[j];
+        __syncthreads();
+        if (threadIdx.x < kJoined) {
+          float all = 0.0f;
+          for (int o = 0; o < waves; ++o) all += s_sum[o][threadIdx.x];
+          const int j = j0 + (int)threadIdx.x;
+          if (j < count) store_weight(a.grad_weights, a.weights_type, token * a.top + first + j, held >> j & 1 ? all : 0.0f);
+        }
+        __syncthreads();
+      } else {
+#pragma unroll
+        for (int j = 0; j < kJoined; ++j)
+          if (lane == j && j0 + j < count) store_weight(a.grad_weights, a.weights_type, token * a.top + first + j0 + j, row[j] >= 0 ? dot[j] : 0.0f);
+      }
     }
-    if (threadIdx.x == 0) store_weight(a.grad_weights, a.weights_type, token * a.top + j, held ? dot : 0.0f);
   }
 }
 
@@ -425,10 +545,11 @@ extern "C" int lutkan_expert_combine_backward(const lutkan_expert_combine_backwa
   BackwardArgs a;
   a.grad = static_cast<const unsigned char *>(p->grad); a.y = static_cast<const unsigned char *>(p->y); a.weights = static_cast<const unsigned char *>(p->weights);
   a.rows = p->rows; a.places = p->places; a.grad_y = static_cast<unsigned char *>(p->grad_y); a.grad_weights = static_cast<unsigned char *>(p->grad_weights);
-  a.y_rows = p->y_rows; a.tokens = p->tokens; a.grad_stride = (int32_t)p->grad_stride; a.y_stride = p->weights ? (int32_t)p->y_stride : 0; a.grad_y_stride = (int32_t)p->grad_y_stride;
+  a.checks = (int32_t)((p->y_rows + 63) / 64);
+  a.y_rows = (int32_t)p->y_rows; a.tokens = (int32_t)p->tokens; a.grad_stride = (int32_t)p->grad_stride; a.y_stride = p->weights ? (int32_t)p->y_stride : 0; a.grad_y_stride = (int32_t)p->grad_y_stride;
   a.top = p->top; a.width = p->width; a.weights_type = (int8_t)p->weights_type; a.rows_bytes = (int8_t)p->rows_bytes; a.places_bytes = (int8_t)p->places_bytes;
   const int threads = 64 * std::min((p->width + 511) / 512, 16);
-  const int64_t groups = p->tokens + (p->y_rows + 63) / 64;
+  const int64_t groups = p->tokens + a.checks;
   if (groups == 0) return LUTKAN_OK;
   if (!lutkan::launch_holds(groups, threads)) return fail(LUTKAN_EUNSUPPORTED, "%s: too many tokens", who);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
