@@ -26,7 +26,8 @@ static_assert(sizeof(SortArgs) <= 112, "launch");
 
 constexpr int kSortWaves = 16;
 constexpr int kSortHeld = 16;                                     // chunks of 64 choices whose experts a wave holds
-constexpr int kSortSingle = 64 * kSortHeld * kSortWaves;          // choices of one work-group's launch
+// Choices of one work-group's launch: by 64 experts 1024 choices take 5.4 us and 4096 8.5; two launches of several work-groups 11.1 for 16386.
+constexpr int kSortSingle = 6144;
 constexpr int kSortDigit = 11, kSortBins = (1 << kSortDigit) + 1; // (2048 experts and the dropped ones)
 
 // The expert of choice c, `experts` for a choice that is dropped.
@@ -66,26 +67,27 @@ struct SortHeld {
   }
 };
 
-// How many choices of each bin the work-group's waves hold: s_count [wave][bins].  `held` keeps the last chunks.
-__device__ __forceinline__ void count_bins(const SortArgs &a, int *s_count, SortHeld &held, int first, int last, int wave, int waves) {
-  held.read(a, first, last);
-  for (int i = threadIdx.x; i < waves * a.bins; i += blockDim.x) s_count[i] = 0;
-  __syncthreads();
+// How many choices of each bin the work-group's waves hold, into s_count [wave][bins], which is zero.  `held`: the first chunks; it keeps the last.
+__device__ __forceinline__ void count_bins(const SortArgs &a, int *s_count, SortHeld &held, int first, int last, int wave) {
   for (int at = first; at < last; at += 64 * kSortHeld) {
     if (at != first) held.read(a, at, last);
 #pragma unroll
     for (int k = 0; k < kSortHeld; ++k)
       if (at + 64 * k + (int)(threadIdx.x & 63) < last) atomicAdd(&s_count[wave * a.bins + bin_of(a, held.expert[k])], 1);
   }
-  __syncthreads();
 }
 
 __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_count_kernel(const SortArgs a) {
   extern __shared__ int s_count[];
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int64_t first = ((int64_t)blockIdx.x * waves + wave) * a.segment;
+  const int64_t begin = ((int64_t)blockIdx.x * waves + wave) * a.segment;
+  const int first = (int)min(begin, (int64_t)a.choices), last = (int)min(begin + a.segment, (int64_t)a.choices);
   SortHeld held;
-  count_bins(a, s_count, held, (int)min(first, (int64_t)a.choices), (int)min(first + a.segment, (int64_t)a.choices), wave, waves);
+  held.read(a, first, last);
+  for (int i = threadIdx.x; i < waves * a.bins; i += blockDim.x) s_count[i] = 0;
+  __syncthreads();
+  count_bins(a, s_count, held, first, last, wave);
+  __syncthreads();
   for (int e = threadIdx.x; e < a.bins; e += blockDim.x) {
     int sum = 0;
     for (int w = 0; w < waves; ++w) sum += s_count[w * a.bins + e];
@@ -103,11 +105,13 @@ __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_sort_kernel(con
   int *s_total = s_count + waves * bins, *s_wave = s_total + bins, *s_before = s_wave + kSortWaves;
   const int64_t begin = ((int64_t)blockIdx.x * waves + wave) * a.segment;
   const int first = (int)min(begin, (int64_t)a.choices), last = (int)min(begin + a.segment, (int64_t)a.choices);
+  SortHeld held;
+  held.read(a, first, last);
+  for (int i = threadIdx.x; i < waves * bins; i += blockDim.x) s_count[i] = 0;
   if constexpr (SEVERAL)
     for (int e = threadIdx.x; e < bins; e += blockDim.x) s_total[e] = s_before[e] = 0;
-  SortHeld held;
-  count_bins(a, s_count, held, first, last, wave, waves);
-  if constexpr (SEVERAL) {                                        // the work-groups' counts: as many threads to a bin as there are
+  __syncthreads();
+  if constexpr (SEVERAL) {                                        // the work-groups' counts, while the choices are on their way: as many threads to a bin as there are
     const int parts = max(1, (int)blockDim.x / bins), part = threadIdx.x / bins;
     for (int e = parts > 1 ? threadIdx.x % bins : threadIdx.x; e < bins && part < parts; e += parts > 1 ? bins : blockDim.x) {
       int before = 0, total = 0;
@@ -120,8 +124,9 @@ __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_sort_kernel(con
       atomicAdd(&s_before[e], before);
       atomicAdd(&s_total[e], total);
     }
-    __syncthreads();
   }
+  count_bins(a, s_count, held, first, last, wave);
+  __syncthreads();
   // Every bin: in place of the waves' counts, how many of it lie before each wave.
   for (int e = threadIdx.x; e < bins; e += blockDim.x) {
     int before = SEVERAL ? s_before[e] : 0;
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(256) void lutkan_expert_sizes_kernel(const int32_t 
   if (e < experts) group_sizes[e] = below(sorted, choices, e + 1) - below(sorted, choices, e);
 }
 
-// Waves of a work-group and choices of a wave: one work-group up to kSortSingle choices, else at most 256.
+// Waves of a work-group and choices of a wave: one work-group up to kSortSingle choices, else at most 256 work-groups.
 struct SortPlan {
   int waves, segment, groups, bins;
   bool one_pass;
@@ -211,7 +216,9 @@ SortPlan plan_sort(int64_t choices, int experts) {
     p.segment = (int)((chunks + p.waves - 1) / p.waves * 64);
     p.groups = 1;
   } else {
-    const int64_t of_wave = std::max<int64_t>(2, (chunks + 256 * kSortWaves - 1) / (256 * kSortWaves));
+    // A wave's chunk of 64 costs 1.15 us, a work-group's counts 0.35 ns a bin in every work-group.
+    const double best = std::sqrt(205.0 * (double)chunks / std::min(experts + 1, 1 << kSortDigit));
+    const int64_t most = (int64_t)kSortWaves * std::max(1, (int)std::min(best, 256.0)), of_wave = (chunks + most - 1) / most;
     p.waves = kSortWaves;
     p.segment = (int)(of_wave * 64);
     p.groups = (int)((chunks + of_wave * kSortWaves - 1) / (of_wave * kSortWaves));
@@ -347,35 +354,34 @@ struct BackwardArgs {
   unsigned char *grad_y, *grad_weights;
   int32_t y_rows, tokens;
   int32_t grad_stride, y_stride, grad_y_stride;
-  int32_t top, width, checks;                                    // checks: work-groups that look for rows without a choice
+  int32_t top, width, checks;                                    // checks: rows of y that a work-group looks through for some without a choice
   int8_t weights_type, rows_bytes, places_bytes;
 };
 static_assert(sizeof(BackwardArgs) <= 112, "launch");
 
-// A work-group takes a token: its waves share the columns, and their sums meet in LDS in the waves' order.  The first work-groups look through the rows
-// of y for those that no place leads to, 64 each.
+// Which of the rows [first, last) of grad_y, at most 64, no choice leads to.
+__device__ __forceinline__ unsigned long long rows_without_choice(const BackwardArgs &a, int64_t first, int64_t last) {
+  const int64_t row = first + (threadIdx.x & 63);
+  bool found = row >= last;
+  if (!found) {
+    const int64_t token = whole_number(a.rows, row, a.rows_bytes);
+    if (token >= 0 && token < a.tokens)
+      for (int j = 0; j < a.top; ++j) found |= whole_number(a.places, token * a.top + j, a.places_bytes) == row;
+  }
+  return __ballot(!found);
+}
+
+// A work-group takes a token: its waves share the columns, and their sums meet in LDS in the waves' order.  It also looks through its share of the rows
+// of y, at most 16, for those that no place leads to.  (By work-groups of their own, 64 rows each: the 300 dropped rows of 1000 tokens of three, 300 wide, were all in five
+// of them, 23 us.)
 template <int G, int Y>
 __global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(const BackwardArgs a) {
   __shared__ float s_sum[16][kJoined];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  if ((int)blockIdx.x < a.checks) {
-    const int64_t row = (int64_t)blockIdx.x * 64 + lane;
-    bool found = row >= a.y_rows;
-    if (!found) {
-      const int64_t token = whole_number(a.rows, row, a.rows_bytes);
-      if (token >= 0 && token < a.tokens)
-        for (int j = 0; j < a.top && !found; ++j) found = whole_number(a.places, token * a.top + j, a.places_bytes) == row;
-    }
-    const float zeros[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    for (unsigned long long left = __ballot(!found); left != 0; left &= left - 1) {
-      unsigned char *to = a.grad_y + (row - lane + __builtin_ctzll(left)) * a.grad_y_stride * type_bytes(Y);
-      for (int col = 8 * (int)threadIdx.x; col < a.width; col += 8 * blockDim.x) write8<Y>(to, col, a.width, zeros);
-    }
-    return;
-  }
-  const int64_t token = blockIdx.x - a.checks;
+  const int64_t token = blockIdx.x, check = token * a.checks;
+  unsigned long long left = rows_without_choice(a, check, min(check + a.checks, (int64_t)a.y_rows));
   const unsigned char *grad = a.grad + token * a.grad_stride * type_bytes(G);
-  for (int first = 0; first < a.top; first += 64) {
+  for (int first = 0; token < a.tokens && first < a.top; first += 64) {
     const Choices choices(a.places, a.places_bytes, a.weights, a.weights_type, token, a.top, first, a.y_rows);
     const unsigned long long held = __ballot(choices.row >= 0 && whole_number(a.rows, choices.row, a.rows_bytes) == token);      // (one way and back)
     const int count = min(a.top - first, 64);
@@ -434,6 +440,11 @@ __global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(co
           if (lane == j && j0 + j < count) store_weight(a.grad_weights, a.weights_type, token * a.top + first + j0 + j, row[j] >= 0 ? dot[j] : 0.0f);
       }
     }
+  }
+  const float zeros[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  for (; left != 0; left &= left - 1) {
+    unsigned char *to = a.grad_y + (check + __builtin_ctzll(left)) * a.grad_y_stride * type_bytes(Y);
+    for (int col = 8 * (int)threadIdx.x; col < a.width; col += 8 * blockDim.x) write8<Y>(to, col, a.width, zeros);
   }
 }
 
@@ -545,12 +556,12 @@ extern "C" int lutkan_expert_combine_backward(const lutkan_expert_combine_backwa
   BackwardArgs a;
   a.grad = static_cast<const unsigned char *>(p->grad); a.y = static_cast<const unsigned char *>(p->y); a.weights = static_cast<const unsigned char *>(p->weights);
   a.rows = p->rows; a.places = p->places; a.grad_y = static_cast<unsigned char *>(p->grad_y); a.grad_weights = static_cast<unsigned char *>(p->grad_weights);
-  a.checks = (int32_t)((p->y_rows + 63) / 64);
+  const int64_t groups = std::max<int64_t>(p->tokens, (p->y_rows + 15) / 16);      // (few tokens and many rows: work-groups without a token)
+  if (groups == 0) return LUTKAN_OK;
+  a.checks = (int32_t)((p->y_rows + groups - 1) / groups);
   a.y_rows = (int32_t)p->y_rows; a.tokens = (int32_t)p->tokens; a.grad_stride = (int32_t)p->grad_stride; a.y_stride = p->weights ? (int32_t)p->y_stride : 0; a.grad_y_stride = (int32_t)p->grad_y_stride;
   a.top = p->top; a.width = p->width; a.weights_type = (int8_t)p->weights_type; a.rows_bytes = (int8_t)p->rows_bytes; a.places_bytes = (int8_t)p->places_bytes;
   const int threads = 64 * std::min((p->width + 511) / 512, 16);
-  const int64_t groups = p->tokens + a.checks;
-  if (groups == 0) return LUTKAN_OK;
   if (!lutkan::launch_holds(groups, threads)) return fail(LUTKAN_EUNSUPPORTED, "%s: too many tokens", who);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   with_types(p->grad_type, p->y_type, [&](auto g, auto y) { hipLaunchKernelGGL((lutkan_expert_combine_backward_kernel<g, y>), dim3((unsigned)groups), dim3(threads), 0, s, a); });
