@@ -282,12 +282,22 @@ __device__ __forceinline__ void write8(unsigned char *row, int col, int width, c
   for (int e = 0; e < 8; ++e) if (col + e < width) store_one<TYPE>(row + (size_t)(col + e) * type_bytes(TYPE), v[e]);
 }
 
-// Eight columns as they lie in memory, asked for and used later; a row that ends inside them is read element by element.
+typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));        // at any address that an element can have
+
+// Eight columns as they lie in memory, asked for and used later; a row that ends inside them is read element by element.  ONCE: nobody else reads the row,
+// and it need not stay in the caches (16384 tokens of four rows of 2048, bf16: joined in 66 -> 60 us, gradients 118 -> 99; of rows that several read 43 -> 49).
 template <int TYPE>
 struct Asked8 {
   Raw8<TYPE> raw;
+  template <bool ONCE>
   __device__ __forceinline__ void ask(const unsigned char *row, int col, int width) {
-    if (col + 8 <= width) raw = load_raw8<TYPE>(row + (size_t)col * type_bytes(TYPE));
+    if (col + 8 > width) return;
+    const u32x4_any *p = reinterpret_cast<const u32x4_any *>(row + (size_t)col * type_bytes(TYPE));
+#pragma unroll
+    for (int h = 0; h < type_bytes(TYPE) / 2; ++h) {
+      if constexpr (ONCE) raw.v[h] = __builtin_nontemporal_load(p + h);
+      else raw.v[h] = p[h];
+    }
   }
   __device__ __forceinline__ void get(const unsigned char *row, int col, int width, float (&v)[8]) const {
     if (col + 8 <= width) values8<TYPE>(raw, v);
@@ -315,8 +325,8 @@ struct Choices {
 
 constexpr int kJoined = 4;                                       // rows that are read before the first is used
 
-// A wave sums 512 columns of one token, eight a lane.
-template <int Y, int O>
+// A wave sums 512 columns of one token, eight a lane.  ONCE: several rows a token, which no other token has.
+template <int Y, int O, bool ONCE>
 __global__ __launch_bounds__(256) void lutkan_expert_combine_kernel(const CombineArgs a) {
   const int lane = threadIdx.x & 63, pieces = (a.width + 511) / 512;
   const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), token = unit / pieces;
@@ -331,7 +341,7 @@ __global__ __launch_bounds__(256) void lutkan_expert_combine_kernel(const Combin
 #pragma unroll
       for (int j = 0; j < kJoined; ++j) {                        // (lanes behind the last choice hold none)
         const int row = j0 + j < 64 ? choices.row_of(j0 + j) : -1;
-        if (row >= 0) asked[j].ask(a.y + row * a.y_stride * type_bytes(Y), col, a.width);
+        if (row >= 0) asked[j].template ask<ONCE>(a.y + row * a.y_stride * type_bytes(Y), col, a.width);
       }
 #pragma unroll
       for (int j = 0; j < kJoined; ++j) {
@@ -354,34 +364,39 @@ struct BackwardArgs {
   unsigned char *grad_y, *grad_weights;
   int32_t y_rows, tokens;
   int32_t grad_stride, y_stride, grad_y_stride;
-  int32_t top, width, checks;                                    // checks: rows of y that a work-group looks through for some without a choice
+  int32_t top, width, checks;                                    // checks: work-groups that look for rows without a choice
   int8_t weights_type, rows_bytes, places_bytes;
 };
 static_assert(sizeof(BackwardArgs) <= 112, "launch");
 
-// Which of the rows [first, last) of grad_y, at most 64, no choice leads to.
-__device__ __forceinline__ unsigned long long rows_without_choice(const BackwardArgs &a, int64_t first, int64_t last) {
-  const int64_t row = first + (threadIdx.x & 63);
-  bool found = row >= last;
-  if (!found) {
-    const int64_t token = whole_number(a.rows, row, a.rows_bytes);
-    if (token >= 0 && token < a.tokens)
-      for (int j = 0; j < a.top; ++j) found |= whole_number(a.places, token * a.top + j, a.places_bytes) == row;
-  }
-  return __ballot(!found);
-}
+constexpr int kCheckRows = 16;                                   // rows of y that a wave looks through, four lanes each
 
-// A work-group takes a token: its waves share the columns, and their sums meet in LDS in the waves' order.  It also looks through its share of the rows
-// of y, at most 16, for those that no place leads to.  (By work-groups of their own, 64 rows each: the 300 dropped rows of 1000 tokens of three, 300 wide, were all in five
-// of them, 23 us.)
+// A work-group takes a token: its waves share the columns, and their sums meet in LDS in the waves' order.  The waves of the first work-groups look
+// through the rows of y for those that no place leads to.  (64 rows a work-group: the 300 dropped rows of 1000 tokens of three, 300 wide, were all in five of
+// them, 23 us for 7.  16 a work-group of four waves: 16384 tokens of four, 2048 wide, 99 -> 112 us; looked for by the tokens' work-groups 99 -> 108.)
 template <int G, int Y>
 __global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(const BackwardArgs a) {
   __shared__ float s_sum[16][kJoined];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const int64_t token = blockIdx.x, check = token * a.checks;
-  unsigned long long left = rows_without_choice(a, check, min(check + a.checks, (int64_t)a.y_rows));
+  if ((int)blockIdx.x < a.checks) {
+    const int64_t first = ((int64_t)blockIdx.x * waves + wave) * kCheckRows, row = first + (lane >> 2);
+    bool found = row >= a.y_rows;
+    if (!found) {
+      const int64_t token = whole_number(a.rows, row, a.rows_bytes);
+      if (token >= 0 && token < a.tokens)
+        for (int j = lane & 3; j < a.top; j += 4) found |= whole_number(a.places, token * a.top + j, a.places_bytes) == row;
+    }
+    const unsigned long long by_four = __ballot(found);
+    const float zeros[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    for (int r = 0; r < kCheckRows; ++r) {
+      if (by_four >> (4 * r) & 15) continue;
+      for (int col = 8 * lane; col < a.width; col += 512) write8<Y>(a.grad_y + (first + r) * a.grad_y_stride * type_bytes(Y), col, a.width, zeros);
+    }
+    return;
+  }
+  const int64_t token = blockIdx.x - a.checks;
   const unsigned char *grad = a.grad + token * a.grad_stride * type_bytes(G);
-  for (int first = 0; token < a.tokens && first < a.top; first += 64) {
+  for (int first = 0; first < a.top; first += 64) {
     const Choices choices(a.places, a.places_bytes, a.weights, a.weights_type, token, a.top, first, a.y_rows);
     const unsigned long long held = __ballot(choices.row >= 0 && whole_number(a.rows, choices.row, a.rows_bytes) == token);      // (one way and back)
     const int count = min(a.top - first, 64);
@@ -396,10 +411,10 @@ __global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(co
       for (int col = 8 * (int)threadIdx.x; col < a.width; col += 8 * blockDim.x) {
         Asked8<G> asked;
         Asked8<Y> of_y[kJoined];
-        asked.ask(grad, col, a.width);
+        asked.template ask<false>(grad, col, a.width);
         if (a.weights)
 #pragma unroll
-          for (int j = 0; j < kJoined; ++j) if (row[j] >= 0) of_y[j].ask(a.y + row[j] * (int64_t)a.y_stride * type_bytes(Y), col, a.width);
+          for (int j = 0; j < kJoined; ++j) if (row[j] >= 0) of_y[j].template ask<true>(a.y + row[j] * (int64_t)a.y_stride * type_bytes(Y), col, a.width);
         float g[8];
         asked.get(grad, col, a.width, g);
 #pragma unroll
@@ -440,11 +455,6 @@ __global__ __launch_bounds__(1024) void lutkan_expert_combine_backward_kernel(co
           if (lane == j && j0 + j < count) store_weight(a.grad_weights, a.weights_type, token * a.top + first + j0 + j, row[j] >= 0 ? dot[j] : 0.0f);
       }
     }
-  }
-  const float zeros[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  for (; left != 0; left &= left - 1) {
-    unsigned char *to = a.grad_y + (check + __builtin_ctzll(left)) * a.grad_y_stride * type_bytes(Y);
-    for (int col = 8 * (int)threadIdx.x; col < a.width; col += 8 * blockDim.x) write8<Y>(to, col, a.width, zeros);
   }
 }
 
@@ -536,7 +546,10 @@ extern "C" int lutkan_expert_combine(const lutkan_expert_combine_args *p, void *
     if (p->weights) a.weights = static_cast<const unsigned char *>(p->weights) + first * p->top * type_bytes(p->weights_type);
     a.out = static_cast<unsigned char *>(p->out) + first * p->out_stride * type_bytes(p->out_type);
     const dim3 groups((unsigned)((a.tokens * pieces + 3) / 4));
-    with_types(p->y_type, p->out_type, [&](auto y, auto o) { hipLaunchKernelGGL((lutkan_expert_combine_kernel<y, o>), groups, dim3(256), 0, s, a); });
+    with_types(p->y_type, p->out_type, [&](auto y, auto o) {
+      if (p->top > 1) hipLaunchKernelGGL((lutkan_expert_combine_kernel<y, o, true>), groups, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((lutkan_expert_combine_kernel<y, o, false>), groups, dim3(256), 0, s, a);
+    });
     if (int rc = check_launch(who)) return rc;
   }
   return LUTKAN_OK;
@@ -556,12 +569,13 @@ extern "C" int lutkan_expert_combine_backward(const lutkan_expert_combine_backwa
   BackwardArgs a;
   a.grad = static_cast<const unsigned char *>(p->grad); a.y = static_cast<const unsigned char *>(p->y); a.weights = static_cast<const unsigned char *>(p->weights);
   a.rows = p->rows; a.places = p->places; a.grad_y = static_cast<unsigned char *>(p->grad_y); a.grad_weights = static_cast<unsigned char *>(p->grad_weights);
-  const int64_t groups = std::max<int64_t>(p->tokens, (p->y_rows + 15) / 16);      // (few tokens and many rows: work-groups without a token)
+  const int threads = 64 * std::min((p->width + 511) / 512, 16);
+  const int64_t check_rows = kCheckRows * threads / 64;
+  a.checks = (int32_t)((p->y_rows + check_rows - 1) / check_rows);
+  const int64_t groups = p->tokens + a.checks;
   if (groups == 0) return LUTKAN_OK;
-  a.checks = (int32_t)((p->y_rows + groups - 1) / groups);
   a.y_rows = (int32_t)p->y_rows; a.tokens = (int32_t)p->tokens; a.grad_stride = (int32_t)p->grad_stride; a.y_stride = p->weights ? (int32_t)p->y_stride : 0; a.grad_y_stride = (int32_t)p->grad_y_stride;
   a.top = p->top; a.width = p->width; a.weights_type = (int8_t)p->weights_type; a.rows_bytes = (int8_t)p->rows_bytes; a.places_bytes = (int8_t)p->places_bytes;
-  const int threads = 64 * std::min((p->width + 511) / 512, 16);
   if (!lutkan::launch_holds(groups, threads)) return fail(LUTKAN_EUNSUPPORTED, "%s: too many tokens", who);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   with_types(p->grad_type, p->y_type, [&](auto g, auto y) { hipLaunchKernelGGL((lutkan_expert_combine_backward_kernel<g, y>), dim3((unsigned)groups), dim3(threads), 0, s, a); });
