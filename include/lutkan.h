@@ -475,9 +475,9 @@ int lutkan_rmsnorm_int8(const lutkan_rmsnorm_fp8_args *args, void *hip_stream);
 int lutkan_quantise_int8(const void *rows, int32_t type, int64_t matrices, int32_t n, int32_t k, int64_t stride, int64_t matrix_stride,
                          void *codes, float *scales, void *hip_stream);
 
-/* y[s][j] = x_scales[s] * weight_scales[j] * sum over k of x[s][k] * weight[j][k].  The sum is exact (32-bit integers); its value times the
- * scales' product is rounded to fp32 (an error of at most 3 2^-24 of y), then to y_type.  Scales may be any numbers: where they or their product leave
- * 2^-60 .. 2^60 the row's tile is scaled in fp64.  Arguments, groups and gathered rows as of lutkan_[grouped_]matmul_fp8, with
+/* y[s][j] = x_scales[s] * weight_scales[j] * sum over k of x[s][k] * weight[j][k].  The sum is exact (32-bit integers); as fp32, times
+ * x_scales[s], times weight_scales[j], each rounded (an error of at most 3 2^-24 of y), then to y_type: equal bits whatever the sizes around the
+ * row and column are.  Scales may be any numbers: an output with one outside 2^-60 .. 2^60 is scaled in fp64.  Arguments, groups and gathered rows as of lutkan_[grouped_]matmul_fp8, with
  * x_scales [x_rows], x_scales_stride elements apart (0: one scale for all), and weight_scales [groups][n], contiguous; a row
  * of zeros (row_index outside x, or behind the last group) is zeros whatever the scales are.
  * Errors as there; k at most LUTKAN_INT8_MAX_INPUTS. */

@@ -19,15 +19,18 @@ __device__ __forceinline__ i32x16 product_32x32(u32x4 w, u32x4 x, i32x16 sum) { 
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, x), sum, 0, 0, 0);
 }
 
-// Scales that fp32 multiplies without loss: a product of two lies in 2^-120 .. 2^120, and times a sum below 2^31 beyond fp32 only where y is.
+// Scales that fp32 multiplies without loss: a sum below 2^31 times two of them lies beyond fp32 only where y does.
 __device__ __forceinline__ bool ordinary(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
 
-// Four sums times their scales; `exact`: in fp64, for scales that are not ordinary (uniform over a wave).
-__device__ __forceinline__ f32x4 scaled(i32x4 sum, float x_scale, f32x4 w_scale, bool exact) {
+// Four sums times the row's scale, then times their own, each rounded; in fp64 where one of the two scales is not ordinary (`any`: some are).  Every kernel does
+// it so, and the sums are exact: an output does not depend on the kernel.
+__device__ __forceinline__ f32x4 scaled(i32x4 sum, float x_scale, f32x4 w_scale, bool any) {
   f32x4 v;
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    v[e] = exact ? (float)((double)sum[e] * ((double)x_scale * (double)w_scale[e])) : (float)sum[e] * (x_scale * w_scale[e]);
+  for (int e = 0; e < 4; ++e) {
+    v[e] = (float)sum[e] * x_scale * w_scale[e];
+    if (any && !(ordinary(x_scale) && ordinary(w_scale[e]))) v[e] = (float)((double)sum[e] * ((double)x_scale * (double)w_scale[e]));
+  }
   return v;
 }
 
@@ -525,70 +528,65 @@ int launch_tiles(const ProductArgs &a, int64_t row_tiles, bool async, const char
   return async ? launch_tiles_as<TM, TN, WM, WN, KG, GROUPED, true>(a, row_tiles, who, s) : launch_tiles_as<TM, TN, WM, WN, KG, GROUPED, false>(a, row_tiles, who, s);
 }
 
-inline double direct_price(double row_tiles, double rows_of_tile, int columns, const ProductArgs &a) {
-  const double work_groups = row_tiles * ((a.n + columns - 1) / columns);
-  return work_groups * (rows_of_tile + columns) * a.k / (9e6 * std::min(1.0, work_groups / 256));
-}
-inline double tiled_price(double tiles, int slots, double one, double all, double ends, double steps, bool guess) {
-  if (guess && slots > 1 && tiles > 256) return std::max(1.0, tiles / (256 * slots)) * (steps * all + ends);
-  const double full = std::floor(tiles / (256 * slots)), rest = tiles - full * 256 * slots;
-  return full * (steps * all + ends) + (rest > 0 ? steps * (rest <= 256 ? one : all) + ends : 0);
-}
+// What a launch takes beyond an empty one (2.4 us in a replayed graph), in us, for the kernels' choice.  The constants were fitted to 650 drawn calls of 1 to
+// 32768 rows, 16 to 8192 inputs and 2 to 8192 outputs, a third of them with rows at odd addresses, half by expert, each timed with every kernel; on 260 others the
+// kernel that is taken was within 2 % of the quickest in 220, 1.02 times it in the geometric mean, 1.5 at worst (few steps of many tiles).  Tried beside these, and
+// not worth their place: direct tiles of 32 x 32, four teams on 64 x 64, two on 128 x 128 (each is the quickest of 1 - 4 % of the calls, by little).
+//   direct   what its work-groups read, each its own, over the whole GPU, and their number
+//   tiled    rounds of as many tiles as fit the compute units, a tile's steps of 128 k: `one` where there is one to a compute unit, `all` where
+//            there are `slots`, and `ends` before and behind the steps.  Where the number of tiles is a guess (groups) and two fit a compute
+//            unit, a round that is begun counts by its part.
+struct Call {
+  const ProductArgs &a;
+  bool grouped, aligned, async;
+  double likely_tiles(int height) const {                        // of a routing of some spread: a group's last tile is half empty
+    if (!grouped) return (double)(((int64_t)a.rows + height - 1) / height);
+    const double some = (double)std::min(a.groups, a.rows), each = (double)a.rows / some;
+    return some * std::max(1.0, each / height + (each > 1 ? 0.6 : 0.0));
+  }
+  double direct(int columns, double base, double rate, double by_expert, double times, double of_work_group) const {
+    const double work_groups = likely_tiles(16) * ((a.n + columns - 1) / columns), rows = std::min(16.0, grouped ? (double)a.rows / std::min(a.groups, a.rows) : (double)a.rows);
+    const double reads = work_groups * (rows + columns) * a.k / (rate * std::min(1.0, work_groups / 256));
+    return base + reads * (aligned ? 1 : 1.6) * (grouped ? times : 1) + (grouped ? by_expert : 0) + of_work_group * std::max(0.0, work_groups - 512);      // (unaligned: five dwords for every four)
+  }
+  double tiled(int height, int width, int slots, int teams, double ends, double one, double all, double search, double end_block) const {
+    const double tiles = likely_tiles(height) * ((a.n + width - 1) / width);
+    const double steps = async ? a.k / 64 / 2.0 / teams : 2.0 * (a.k / 128) / teams;      // (through registers a step takes twice as long)
+    ends += (grouped ? search : 0) + (a.k % (async ? 64 : 128) ? end_block : 0);
+    if (grouped && slots > 1 && tiles > 256) return std::max(1.0, tiles / (256 * slots)) * (steps * all + ends);
+    const double full = std::floor(tiles / (256 * slots)), rest = tiles - full * 256 * slots;
+    return full * (steps * all + ends) + (rest > 0 ? steps * (rest <= 256 ? one : all) + ends : 0);
+  }
+};
 
 template <bool GROUPED>
 int launch_product(const ProductArgs &a, const char *who, hipStream_t s) {
-  const int64_t groups = GROUPED ? a.groups : 1;
   const auto tiles = [&](int height) {                           // no routing has more
-    return GROUPED ? a.rows / height + std::min<int64_t>(groups + 1, a.rows) : ((int64_t)a.rows + height - 1) / height;
-  };
-  const auto likely_tiles = [&](int height) {                    // of a routing of some spread: a group's last tile is half empty
-    if (!GROUPED) return (double)tiles(height);
-    const double some = (double)std::min<int64_t>(groups, a.rows), each = (double)a.rows / some;
-    return some * std::max(1.0, each / height + (each > 1 ? 0.6 : 0.0));
+    return GROUPED ? a.rows / height + (int64_t)std::min(a.groups + 1, a.rows) : ((int64_t)a.rows + height - 1) / height;
   };
   lutkan::plan_clear();
   const bool aligned = rows_aligned(a), async = aligned && copies_fit<GROUPED>(a);
-  const double likely_rows = (double)a.rows / (double)std::min<int64_t>(groups, a.rows);
-  const double end_block = a.k % kScaleBlock ? 2.5 : 0;          // (read, put and multiplied behind the others)
-  const auto tiled = [&](int side, int slots, double one, double all, double ends, int teams) {
-    const double step = async ? 1 : side == 64 ? 1.75 : 1.5;     // (through registers a step waits longer)
-    return tiled_price(likely_tiles(side) * ((a.n + side - 1) / side), slots, one * step, all * step, ends + end_block, std::ceil(a.k / kScaleBlock / (double)teams), GROUPED);
-  };
-  enum { kDirect16x16, kDirect16x32, kDirect32x32, kTiled64x4, kTiled64x2, kTiled128x2, kTiled128, kTiled256, kTiled128x256, kKernels };
+  const Call call{a, GROUPED, aligned, async};
+  enum { kDirect16x16, kDirect16x32, kTiled64, kTiled128, kTiled128x256, kTiled256, kKernels };
   double price[kKernels];
-  price[kDirect16x16] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 16, a);
-  price[kDirect16x32] = direct_price(likely_tiles(16), std::min(16.0, likely_rows), 32, a);
-  price[kDirect32x32] = direct_price(likely_tiles(32), std::min(32.0, likely_rows), 32, a);
-  constexpr double kSearch = GROUPED ? 2 : 0;                    // for the group, before a small tile's few steps
-  price[kTiled64x4] = tiled(64, 1, 0.62, 1.0, 1 + kSearch, 4);
-  price[kTiled64x2] = tiled(64, 2, 0.36, 0.85, 1 + kSearch, 2);
-  price[kTiled128x2] = tiled(128, 1, 1.0, 1.0, 5, 2);
-  price[kTiled128] = tiled(128, 2, 0.65, 1.08, 2, 1);
-  price[kTiled256] = tiled(256, 1, 1.3, 1.3, 6, 1);
-  price[kTiled128x256] = async ? 1e300 : HUGE_VAL;
-  if (GROUPED)                                                   // (weights that few rows share come from memory)
-    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 1.7;
-  if (!aligned)                                                  // (five dwords for every four)
-    for (int k = kDirect16x16; k <= kDirect32x32; ++k) price[k] *= 2;
-  if (!async) price[kTiled256] = HUGE_VAL;                       // (its sums leave no registers to copy through)
+  price[kDirect16x16] = call.direct(16, 0.6, 9.8e6, 0.57, 1.58, 0.39e-3);
+  price[kDirect16x32] = call.direct(32, 0.93, 11.6e6, 0.64, 1.44, 0.64e-3);
+  price[kTiled64] = call.tiled(64, 64, 2, 2, 1.47, 0.416, 1.0, 1.0, 1.1);
+  price[kTiled128] = call.tiled(128, 128, 2, 1, 2.54, 0.469, 1.31, 0.93, 2.2);
+  price[kTiled128x256] = async ? call.tiled(128, 256, 2, 1, 4.6, 0.78, 2.43, 0.2, 1.8) : HUGE_VAL;      // (the sums of these two leave no registers to copy through)
+  price[kTiled256] = async ? call.tiled(256, 256, 1, 1, 5.6, 1.17, 1.94, 0, 1.7) : HUGE_VAL;
   if (tiles(16) > 65535) price[kDirect16x16] = price[kDirect16x32] = HUGE_VAL;
-  if (tiles(32) > 65535) price[kDirect32x32] = HUGE_VAL;
-  const auto beyond_a_launch = [&](int side, int threads) { return !lutkan::launch_holds(tiles(side) * ((a.n + side - 1) / side), threads); };
-  if (beyond_a_launch(64, 1024)) price[kTiled64x4] = HUGE_VAL;
-  if (beyond_a_launch(64, 512)) price[kTiled64x2] = HUGE_VAL;
-  if (beyond_a_launch(128, 512)) price[kTiled128x2] = HUGE_VAL;
-  if (beyond_a_launch(128, 256)) price[kTiled128] = HUGE_VAL;
-  if (beyond_a_launch(256, 512)) price[kTiled256] = HUGE_VAL;
-  if (!lutkan::launch_holds(tiles(128) * ((a.n + 255) / 256), 256)) price[kTiled128x256] = HUGE_VAL;
+  const auto beyond_a_launch = [&](int height, int width, int threads) { return !lutkan::launch_holds(tiles(height) * ((a.n + width - 1) / width), threads); };
+  if (beyond_a_launch(64, 64, 512)) price[kTiled64] = HUGE_VAL;
+  if (beyond_a_launch(128, 128, 256)) price[kTiled128] = HUGE_VAL;
+  if (beyond_a_launch(128, 256, 256)) price[kTiled128x256] = HUGE_VAL;
+  if (beyond_a_launch(256, 256, 512)) price[kTiled256] = HUGE_VAL;
   const int pick = (int)(std::min_element(price, price + kKernels) - price);
   if (price[pick] == HUGE_VAL) return fail(LUTKAN_EUNSUPPORTED, "%s: too many outputs", who);
   switch (pick) {
     case kDirect16x16: return launch_direct<1, 1, GROUPED>(a, tiles(16), aligned, who, s);
     case kDirect16x32: return launch_direct<1, 2, GROUPED>(a, tiles(16), aligned, who, s);
-    case kDirect32x32: return launch_direct<2, 2, GROUPED>(a, tiles(32), aligned, who, s);
-    case kTiled64x4: return launch_tiles<1, 1, 2, 2, 4, GROUPED>(a, tiles(64), async, who, s);
-    case kTiled64x2: return launch_tiles<1, 1, 2, 2, 2, GROUPED>(a, tiles(64), async, who, s);
-    case kTiled128x2: return launch_tiles<2, 2, 2, 2, 2, GROUPED>(a, tiles(128), async, who, s);
+    case kTiled64: return launch_tiles<1, 1, 2, 2, 2, GROUPED>(a, tiles(64), async, who, s);
     case kTiled128x256: return launch_tiles_as<2, 4, 2, 2, 1, GROUPED, true>(a, tiles(128), who, s);
     case kTiled256: return launch_tiles_as<4, 2, 2, 4, 1, GROUPED, true>(a, tiles(256), who, s);
     default: return launch_tiles<2, 2, 2, 2, 1, GROUPED>(a, tiles(128), async, who, s);

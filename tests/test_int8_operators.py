@@ -1,7 +1,7 @@
 """The operators on 8-bit integers against their definition in 64 bits (numpy, on the CPU).
 
 Bounds, from the arithmetic (u = 2^-24, half a step of fp32):
-  product     the sum is a whole number below 2^31, held exactly; made fp32, times the product of both scales: three roundings, 3 u of y (in fp64 for
+  product     the sum is a whole number below 2^31, held exactly; made fp32, times one scale, times the other: three roundings, 3 u of y (in fp64 for
               scales outside 2^-60 .. 2^60: one, u).  Then the rounding of the output, half a step of its type.
   rows        the scale is one division, rounded; a code is off value / scale by half and by the quotient's rounding, 2 u of it
   norm        a sum of squares of `width` terms, root, products: (width + 16) u relative for y and the scale; a code is off y / scale by half and that
