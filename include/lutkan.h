@@ -492,7 +492,7 @@ int lutkan_grouped_matmul_int8(const lutkan_matmul_fp8_args *args, void *hip_str
  *   rows         [tokens * top]   the token of each sorted row (what row_index of a grouped product takes); -1 behind the last group
  *   places       [tokens][top]    the sorted row of each choice; -1: dropped
  *   group_sizes  [experts]
- * workspace: device, >= lutkan_expert_sort_workspace_bytes(tokens, top, experts) (0 for the smaller calls, one launch: up to 6144 choices of 2048 experts), 4-byte
+ * workspace: device, >= lutkan_expert_sort_workspace_bytes(tokens, top, experts) (0 for the smaller calls, one launch: up to 4096 choices of 2048 experts), 4-byte
  * aligned, free again once the call's kernels have run.
  * Errors: EINVAL, ESHAPE (workspace, stride), EUNSUPPORTED (experts, choices), EHIP. */
 typedef struct {

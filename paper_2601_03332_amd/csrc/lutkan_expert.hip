@@ -25,9 +25,11 @@ struct SortArgs {
 static_assert(sizeof(SortArgs) <= 112, "launch");
 
 constexpr int kSortWaves = 16;
-constexpr int kSortHeld = 16;                                     // chunks of 64 choices whose experts a wave holds
-// Choices of one work-group's launch: by 64 experts 1024 choices take 5.4 us and 4096 8.5; two launches of several work-groups 11.1 for 16386.
-constexpr int kSortSingle = 6144;
+// Chunks of 64 choices whose experts a wave holds; their loop is unrolled, and a longer code costs more to fetch than it saves (with 16 of them 524288 choices take
+// 16.2 us for 13.3, one token 3.9 for 3.3).
+constexpr int kSortHeld = 4;
+// Choices of one work-group's launch: 4080 of 64 experts take 7.8 us and 4800 10.2, two launches of several work-groups 8.4 for these.
+constexpr int kSortSingle = 64 * kSortHeld * kSortWaves;
 constexpr int kSortDigit = 11, kSortBins = (1 << kSortDigit) + 1; // (2048 experts and the dropped ones)
 
 // The expert of choice c, `experts` for a choice that is dropped.
@@ -216,8 +218,9 @@ SortPlan plan_sort(int64_t choices, int experts) {
     p.segment = (int)((chunks + p.waves - 1) / p.waves * 64);
     p.groups = 1;
   } else {
-    // A wave's chunk of 64 costs 1.15 us, a work-group's counts 0.35 ns a bin in every work-group.
-    const double best = std::sqrt(205.0 * (double)chunks / std::min(experts + 1, 1 << kSortDigit));
+    // More work-groups are shorter, and each reads the counts of all: 524288 choices of 256 experts take 21.2 us with 81 of them, 16.9 with 160; of 64
+    // experts 17.6, 13.4 and 12.8 with 112, 160 and 256.
+    const double best = std::sqrt(800.0 * (double)chunks / std::min(experts + 1, 1 << kSortDigit));
     const int64_t most = (int64_t)kSortWaves * std::max(1, (int)std::min(best, 256.0)), of_wave = (chunks + most - 1) / most;
     p.waves = kSortWaves;
     p.segment = (int)(of_wave * 64);

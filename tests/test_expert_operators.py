@@ -44,7 +44,7 @@ def sort_reference(expert, experts):
     return rows.int(), places.view(expert.shape).int(), torch.bincount(key, minlength=experts + 1)[:experts].int()
 
 
-SORTS = [(1, 1, 1), (1, 2, 8), (3, 1, 5), (7, 8, 8), (16, 2, 8), (64, 1, 64), (65, 1, 3), (33, 2, 63), (500, 3, 12), (1023, 1, 65), (1024, 16, 128), (4097, 4, 256), (2048, 3, 64), (2049, 3, 64),
+SORTS = [(1, 1, 1), (1, 2, 8), (3, 1, 5), (7, 8, 8), (16, 2, 8), (64, 1, 64), (65, 1, 3), (33, 2, 63), (500, 3, 12), (1023, 1, 65), (1024, 16, 128), (4097, 4, 256), (2048, 2, 64), (2049, 2, 64),
          (2049, 8, 2048), (16384, 1, 2), (16385, 1, 33), (16384, 8, 64), (100003, 3, 7), (3, 40000, 100), (300000, 2, 1000),
          (5, 3, 2049), (8000, 2, 4096), (9000, 2, 2047), (40000, 2, 70001), (3000, 4, 1 << 20)]
 
@@ -365,7 +365,7 @@ def test_the_library_refuses_bad_arguments():
     _refused(-2, sort(expert_stride=-1))
     _refused(-5, sort(experts=(1 << 20) + 1))
     _refused(-5, sort(tokens=(1 << 23) + 1))
-    assert lib.lutkan_expert_sort_workspace_bytes(1000, 6, 8) == 0 and lib.lutkan_expert_sort_workspace_bytes(100000, 2, 8) > 0
+    assert lib.lutkan_expert_sort_workspace_bytes(1024, 4, 2048) == 0 and lib.lutkan_expert_sort_workspace_bytes(100000, 2, 8) > 0
     for bad in ((-1, 2, 8), (5, 0, 8), (5, 2, 0), (5, 2, (1 << 20) + 1), (1 << 40, 2, 8)):
         assert lib.lutkan_expert_sort_workspace_bytes(*bad) == 0
 
