@@ -68,6 +68,12 @@ __global__ __launch_bounds__(1024) void lutkan_int8_direct_kernel(const ProductA
   int64_t from[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) from[m] = t.group < 0 ? -1 : source_row<GROUPED>(a, min(t.first + 16 * m + (lane & 15), t.end - 1));
+  float xs[MT];                                                  // (asked for before the codes: at the end they would be waited for)
+  f32x4 ws[NT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) xs[m] = from[m] >= 0 ? a.x_scales[from[m] * a.x_scales_stride] : 1.0f;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) ws[n] = weight_scales(a, max(t.group, 0), col0 + 16 * n + 4 * p);
   if (t.group >= 0) {
     const unsigned char *x[MT], *w[NT];
 #pragma unroll
@@ -141,10 +147,8 @@ __global__ __launch_bounds__(1024) void lutkan_int8_direct_kernel(const ProductA
       const int64_t row = t.first + 16 * m + (lane & 15);
       const int col = col0 + 16 * n + 4 * p;
       f32x4 y{0.0f, 0.0f, 0.0f, 0.0f};
-      const float xs = from[m] >= 0 ? a.x_scales[from[m] * a.x_scales_stride] : 1.0f;
-      const f32x4 ws = weight_scales(a, max(t.group, 0), col);
-      const bool exact = !__all(ordinary(xs) && ordinary(ws[0]) && ordinary(ws[1]) && ordinary(ws[2]) && ordinary(ws[3]));
-      if (from[m] >= 0) y = scaled(v, xs, ws, exact);
+      const bool any = !__all(ordinary(xs[m]) && ordinary(ws[n][0]) && ordinary(ws[n][1]) && ordinary(ws[n][2]) && ordinary(ws[n][3]));
+      if (from[m] >= 0) y = scaled(v, xs[m], ws[n], any);
       if (row < t.end) store_outputs(a, row, col, y);
     }
 }
