@@ -191,26 +191,37 @@ __device__ __forceinline__ void store_some(const ProductArgs &a, int64_t row, in
   }
 }
 
+// What they are scaled with, asked for before the codes: at the end it would be waited for.
+template <int TM, int TN, bool GROUPED>
+struct WaveScales {
+  float xs[TM];                                                  // of row 32 m + lane % 32; 0: a row of zeros
+  f32x4 ws[2];                                                   // of the lane's columns (store_wave)
+  bool fine = true;
+  __device__ __forceinline__ WaveScales(const ProductArgs &a, const RowTile &t, int64_t row0, int col0) {
+    const int lane = threadIdx.x & 63, cols = a.y_type == LUTKAN_F32 ? 4 : 8, col = col0 + lane * cols % (32 * TN);
+#pragma unroll
+    for (int m = 0; m < TM; ++m) {
+      const int64_t from = t.group < 0 ? -1 : source_row<GROUPED>(a, min(row0 + 32 * m + (lane & 31), t.end - 1));
+      xs[m] = from >= 0 ? a.x_scales[from * a.x_scales_stride] : 0.0f;
+      fine = fine && (from < 0 || ordinary(xs[m]));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ws[i] = weight_scales(a, max(t.group, 0), col + 4 * i);
+  }
+};
+
 template <int TYPE, int TM, int TN, bool GROUPED>
-__device__ __forceinline__ void store_wave(const ProductArgs &a, const RowTile &t, const i32x16 (&acc)[TM][TN], int64_t row0, int col0, unsigned char *dump) {
+__device__ __forceinline__ void store_wave(const ProductArgs &a, const RowTile &t, const i32x16 (&acc)[TM][TN], int64_t row0, int col0, unsigned char *dump, const WaveScales<TM, TN, GROUPED> &scales) {
   constexpr int kCols = TYPE == LUTKAN_F32 ? 4 : 8, kLanes = 32 * TN / kCols, kRows = 64 / kLanes;       // columns of a lane, lanes of a row, rows at a time
   const int lane = threadIdx.x & 63, col = col0 + lane % kLanes * kCols;
   const int64_t last = t.end - 1;
-  float xs[TM];                                                  // of row 32 m + lane % 32; 0: a row of zeros
-  bool fine = true;
+  const auto &xs = scales.xs;
+  const auto &ws = scales.ws;
+  bool fine = scales.fine;
 #pragma unroll
-  for (int m = 0; m < TM; ++m) {
-    const int64_t from = t.group < 0 ? -1 : source_row<GROUPED>(a, min(row0 + 32 * m + (lane & 31), last));
-    xs[m] = from >= 0 ? a.x_scales[from * a.x_scales_stride] : 0.0f;
-    fine = fine && (from < 0 || ordinary(xs[m]));
-  }
-  f32x4 ws[kCols / 4];
-#pragma unroll
-  for (int i = 0; i < kCols / 4; ++i) {
-    ws[i] = weight_scales(a, max(t.group, 0), col + 4 * i);
+  for (int i = 0; i < kCols / 4; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) fine = fine && ordinary(ws[i][e]);
-  }
   const bool exact = !__all(fine);                               // (then the sums change places, and not their products with xs)
   unsigned char *const to = dump + (lane & 31) * dump_pitch(TN) + (lane >> 5) * 16;
   const unsigned char *const from = dump + lane / kLanes * dump_pitch(TN) + lane % kLanes * kCols * 4;
@@ -319,6 +330,9 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
     t.group = 0;
   }
   if (t.end <= t.first) return;
+  const int64_t row0 = t.first + wm * TM * 32;
+  const int wave_col0 = col0 + wn * TN * 32;
+  const WaveScales<TM, TN, GROUPED> scales(a, t, row0, wave_col0);
   i32x16 acc[TM][TN];
 #pragma unroll
   for (int m = 0; m < TM; ++m)
@@ -506,12 +520,10 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG >= 16 ? 4 : 2) void
   if (KG > 1 && team > 0) return;
   if constexpr (KG == 1) lds_barrier();                          // nobody reads the buffers any more
   unsigned char *const dump = s_tiles + T::kParts + wave * dump_bytes(TN);
-  const int64_t row0 = t.first + wm * TM * 32;
-  const int wave_col0 = col0 + wn * TN * 32;
   switch (a.y_type) {
-    case LUTKAN_F32: store_wave<LUTKAN_F32, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump); break;
-    case LUTKAN_F16: store_wave<LUTKAN_F16, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump); break;
-    default: store_wave<LUTKAN_BF16, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump); break;
+    case LUTKAN_F32: store_wave<LUTKAN_F32, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump, scales); break;
+    case LUTKAN_F16: store_wave<LUTKAN_F16, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump, scales); break;
+    default: store_wave<LUTKAN_BF16, TM, TN, GROUPED>(a, t, acc, row0, wave_col0, dump, scales); break;
   }
 }
 
