@@ -508,7 +508,8 @@ size_t lutkan_expert_sort_workspace_bytes(int64_t tokens, int32_t top, int32_t e
 int lutkan_expert_sort(const lutkan_expert_sort_args *args, void *hip_stream);
 
 /* out[t] = sum over j of weights[t][j] * y[places[t][j]], in the order of j and in fp32, rounded once to out_type.  A place outside
- * [0, y_rows) adds nothing, whatever its weight is; a token without a place is zeros.  weights null: 1.  With top = 1 and places = the rows of lutkan_expert_sort
+ * [0, y_rows) adds nothing, whatever its weight is; a token without a place is zeros.  weights null: 1.  out and y must
+ * not overlap.  With top = 1 and places = the rows of lutkan_expert_sort
  * it brings the tokens into the experts' order; the gradient of that is the same call without weights on the places.
  * Errors: EINVAL, ESHAPE (strides, rows), EUNSUPPORTED (strides, counts), EHIP. */
 typedef struct {
@@ -526,7 +527,8 @@ int lutkan_expert_combine(const lutkan_expert_combine_args *args, void *hip_stre
 /* Its gradients: grad_y[places[t][j]] = weights[t][j] * grad[t] and grad_weights[t][j] = <grad[t], y[places[t][j]]>, products and sums in fp32, rounded
  * once.  places and rows are of one lutkan_expert_sort (rows: the token of each row of y): a place counts where rows leads back to its token;
  * rows of grad_y that no place leads to are zeros, and so is grad_weights of a choice without a place.  Several places must not be equal.
- * Without weights, y is not read and grad_weights not written: both null.  y and grad_y have one type, weights and grad_weights too.
+ * Without weights, y is not read and grad_weights not written: both null.  The outputs
+ * must not overlap the inputs.  y and grad_y have one type, weights and grad_weights too.
  * The order of the sums depends on the sizes, not on the run: equal calls give equal bits.  Errors as lutkan_expert_combine. */
 typedef struct {
   const void *grad;                         /* device [tokens][width] of grad_type */

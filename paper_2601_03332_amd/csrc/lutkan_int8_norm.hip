@@ -327,8 +327,10 @@ extern "C" int lutkan_quantise_int8(const void *rows, int32_t type, int64_t matr
   RowArgs a{};
   a.x = static_cast<const unsigned char *>(rows); a.codes = static_cast<unsigned char *>(codes); a.scales = scales;
   a.width = k; a.x_stride = (int32_t)stride; a.codes_stride = k; a.scales_stride = 1;
-  // Matrices that follow each other at the distance of their rows are one.
-  const bool one = matrices == 1 || (matrix_stride == (int64_t)n * stride && matrices <= INT64_MAX / n / (int64_t)(4 * std::max<int64_t>(stride, k)));
+  // Matrices that follow each other at the distance of their rows are one, and so are those of a single row.
+  const bool single = n == 1 && matrix_stride <= INT32_MAX;
+  const bool one = single || matrices == 1 || (matrix_stride == (int64_t)n * stride && matrices <= INT64_MAX / n / (int64_t)(4 * std::max<int64_t>(stride, k)));
+  if (single && matrices > 1) a.x_stride = (int32_t)matrix_stride;
   a.rows = one ? matrices * n : n;
   for (int64_t m = 0; m < (one ? 1 : matrices); ++m) {
     if (int rc = launch_rows(a, type, false, 0, who, static_cast<hipStream_t>(hip_stream))) return rc;

@@ -332,6 +332,8 @@ def test_the_block_joins_as_torch_does(tokens, codes):
     back = torch.empty((tokens * top, width), device=DEV)
     back[order] = lk.lutkan_forward(layer, z)
     assert torch.equal(y, (back.view(tokens, top, width) * p[..., None]).sum(dim=1).to(x.dtype)) and torch.equal(res, r)
+    none, _ = block(torch.zeros((0, width), device=DEV), torch.zeros((0, width), device=DEV))
+    assert none.shape == (0, width)
     # and how far the unquantised projections are: 8 bits hold a projection to a few percent
     h = x.float() + residual
     n = h * torch.rsqrt(h.square().mean(dim=1, keepdim=True) + block.eps) * norm

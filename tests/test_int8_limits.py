@@ -77,6 +77,38 @@ def test_each_kernel(case):
         assert torch.equal(got, ref.float().to(dtype))
 
 
+# tile, rows, k, n, groups: no block of k to a few more than the buffers, and a last one that is not whole
+SHORT = [("64 columns=64", 6519, 36, 304, 0), ("64 columns=64", 349, 64, 5329, 0), ("64 columns=64", 8173, 100, 227, 0), ("64 columns=64", 4093, 128, 232, 0),
+         ("64 columns=64", 7388, 192, 112, 0), ("64 columns=64", 2507, 200, 670, 0), ("64 columns=64", 1150, 256, 822, 0), ("64 columns=64", 519, 320, 1671, 0),
+         ("64 columns=64", 2277, 384, 390, 0), ("64 columns=64", 210, 448, 3313, 0), ("64 columns=64", 971, 512, 899, 0), ("128 columns=128", 7234, 36, 2118, 0),
+         ("128 columns=128", 3902, 64, 4183, 0), ("128 columns=128", 4331, 100, 1825, 0), ("128 columns=128", 4701, 128, 1641, 0), ("128 columns=128", 4187, 192, 3872, 0),
+         ("128 columns=128", 7546, 200, 2094, 0), ("128 columns=128", 5924, 256, 2594, 0), ("128 columns=128", 3872, 320, 4200, 0), ("128 columns=128", 5462, 384, 2923, 0),
+         ("128 columns=128", 7569, 448, 2136, 0), ("128 columns=128", 2017, 512, 1969, 0), ("128 columns=256", 4852, 36, 3982, 5), ("128 columns=256", 4478, 64, 4237, 5),
+         ("128 columns=256", 7827, 100, 2493, 5), ("128 columns=256", 3808, 128, 5047, 5), ("128 columns=256", 4569, 192, 4285, 5), ("128 columns=256", 3033, 200, 5767, 5),
+         ("128 columns=256", 3205, 256, 5625, 5), ("128 columns=256", 3348, 320, 5791, 5), ("128 columns=256", 3375, 384, 5098, 5), ("128 columns=256", 5330, 448, 3719, 5),
+         ("128 columns=256", 3657, 512, 5033, 5), ("256 columns=256", 7264, 128, 1666, 5), ("256 columns=256", 7880, 192, 1711, 5), ("256 columns=256", 7476, 200, 1440, 5),
+         ("256 columns=256", 6496, 256, 2043, 5), ("256 columns=256", 5572, 320, 2397, 5), ("256 columns=256", 6413, 384, 1977, 5), ("256 columns=256", 2141, 448, 5506, 5),
+         ("256 columns=256", 3807, 512, 3532, 5)]
+
+
+@gpu
+@pytest.mark.parametrize("case", SHORT, ids=lambda c: "-".join(str(v) for v in c))
+def test_rows_of_few_blocks_in_each_tiled_kernel(case):
+    tile, rows, k, n, groups = case
+    print(f"case short {case}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(rows + k)
+    x, w = codes(gen, rows, k), codes(gen, *([groups] if groups else []), n, k)
+    if not groups:
+        y, ref = lk.lutkan_matmul_int8(x, torch.ones(rows, device=DEV), w, torch.ones(n, device=DEV)), x.double() @ w.double().t().contiguous()
+    else:
+        sizes = [rows // groups] * (groups - 1) + [rows - rows // groups * (groups - 1) - 7]
+        y = lk.lutkan_grouped_matmul_int8(x, torch.ones(rows, device=DEV), w, torch.ones(groups, n, device=DEV), torch.tensor(sizes, device=DEV))
+        parts = [v.double() @ w[g].double().t().contiguous() for g, v in enumerate(x.split(sizes + [7])[:groups])]
+        ref = torch.cat(parts + [torch.zeros(7, n, dtype=torch.float64, device=DEV)])
+    assert f"int8_tiled rows={tile}" in lk.lutkan_last_plan(), lk.lutkan_last_plan()
+    assert torch.equal(y.double(), ref)
+
+
 @gpu
 @pytest.mark.parametrize("shape", [(40, 300, 70), (1030, 640, 1290), (4100, 260, 2050)], ids=str)
 def test_an_output_does_not_depend_on_the_rows_and_columns_around_it(shape):

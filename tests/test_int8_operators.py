@@ -234,7 +234,7 @@ def test_rows_of_ties_zeros_tiny_huge_and_not_finite_values():
 @gpu
 def test_rows_of_strided_and_repeated_matrices():
     v = torch.randn(5, 40, 333, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
-    for part in (v[:, :, 3:130], v[:, 5:20], v[1:2].expand(6, 40, 333), v[:, :1, 1:], v[:3, :, :1]):
+    for part in (v[:, :, 3:130], v[:, 5:20], v[1:2].expand(6, 40, 333), v[:, :1, 1:], v[:3, :, :1], v[:, 3:4, :].expand(5, 6, 333), v.transpose(0, 1)):
         codes, scales = lk.lutkan_quantise_int8(part)
         again = lk.lutkan_quantise_int8(part.contiguous())
         assert torch.equal(codes, again[0]) and torch.equal(scales, again[1]) and codes.is_contiguous()
