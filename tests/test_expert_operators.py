@@ -443,3 +443,88 @@ def test_the_binding_refuses_operands_that_do_not_fit():
     _raises("rows must", lk.lutkan_expert_combine_backward, grad, y, rows[:7], e)
     _raises("places must", lk.lutkan_expert_combine_backward, grad, y, rows, e[:3])
     _raises("weights must", lk.lutkan_expert_combine_backward, grad, y, rows, e, torch.ones(4, 1, device=DEV))
+
+
+# ---------------------------------------------------------------- the binding's two paths
+def _every_call(t):
+    """Each operator of this file and of the integer ones, without an output of the caller's; the tensors are made on the first call."""
+    rows, width = t.shape
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    e = torch.randint(-1, 4, (rows, 2), generator=gen, device=DEV)
+    r, places, sizes = lk.lutkan_expert_sort(e, 4)
+    y, p = torch.randn(2 * rows, width, generator=gen, device=DEV), torch.rand(rows, 2, generator=gen, device=DEV)
+    weight, grad = torch.ones(width, device=DEV), torch.randn(rows, width, generator=gen, device=DEV)
+    w, ws = lk.lutkan_quantise_int8(torch.randn(4, 20, width, generator=gen, device=DEV))
+    x, xs = lk.lutkan_quantise_int8(t)
+    return [lambda f, v: f("expert_sort", (v[:, :2] > 0).long(), 4), lambda f, v: f("expert_sort", (v[:, :3] * 3).int(), 3000), lambda f, v: f("expert_combine", y, places, v[:, :2].contiguous(), torch.bfloat16),
+            lambda f, v: f("expert_combine", v, r[:, None], None, None), lambda f, v: f("expert_combine_backward", v, y, r, places, p),
+            lambda f, v: f("expert_combine_backward", grad, y, r, places, v[:, :2].contiguous()), lambda f, v: f("expert_combine_backward", v, y, r, places, None),
+            lambda f, v: f("rmsnorm_int8", v, weight, None, 1e-6), lambda f, v: f("rmsnorm_int8", t, weight, v, 1e-6), lambda f, v: f("quantise_int8", v),
+            lambda f, v: f("matmul_int8", x, v[:, 0].contiguous(), w[0], ws[0], torch.float32), lambda f, v: f("matmul_int8", x, v[:, 1], w, ws, torch.bfloat16, sizes, r)]
+
+
+PUBLIC = {"expert_sort": lk.lutkan_expert_sort, "expert_combine": lambda y, places, w, dtype: lk.lutkan_expert_combine(y, places, w, dtype=dtype),
+          "expert_combine_backward": lk.lutkan_expert_combine_backward, "rmsnorm_int8": lambda x, w, r, eps: lk.lutkan_rmsnorm_int8(x, w, residual=r, eps=eps),
+          "quantise_int8": lk.lutkan_quantise_int8,
+          "matmul_int8": lambda x, xs, w, ws, dtype, *g: lk.lutkan_grouped_matmul_int8(x, xs, w, ws, g[0], rows=g[1], dtype=dtype) if g else lk.lutkan_matmul_int8(x, xs, w, ws, dtype=dtype)}
+
+
+def _plain(out):
+    return [o for o in (out if isinstance(out, tuple) else (out,)) if o is not None]
+
+
+@gpu
+def test_the_general_path_returns_what_the_native_calls_do(monkeypatch):
+    t = torch.randn(37, 130, device=DEV)
+    calls = _every_call(t)
+    native = [_plain(call(lambda name, *args: getattr(binding._native_calls(), name)(*args), t)) for call in calls]
+    monkeypatch.setattr(binding, "_native", binding._GeneralPath)
+    for call, expected in zip(calls, native):
+        got = _plain(call(lambda name, *args: PUBLIC[name](*args), t))
+        assert len(got) == len(expected) and all(a.dtype == b.dtype and torch.equal(a, b) for a, b in zip(got, expected))
+
+
+@gpu
+def test_native_calls_leave_deferred_and_traced_operators_to_the_general_path():
+    from torch._subclasses import FakeTensorMode
+    from torch.utils._python_dispatch import TorchDispatchMode
+    native = binding._native_calls()
+    t = torch.randn(12, 256, device=DEV)
+    calls = _every_call(t)
+
+    def direct(name, *args):
+        return getattr(native, name)(*args)
+    expect = [_plain(call(direct, t)) for call in calls]
+    with torch.inference_mode():
+        for call, y in zip(calls, expect):
+            got = _plain(call(direct, t))
+            assert all(torch.equal(a, b) for a, b in zip(got, y)) and all(a.is_inference() for a in got)
+    watched = t.clone().requires_grad_()                          # (no part in autograd: outputs do not require gradients)
+    for call, y in zip(calls, expect):
+        got = _plain(call(direct, watched))
+        assert all(torch.equal(a, b) and not a.requires_grad for a, b in zip(got, y))
+
+    class Passes(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+    taken = []
+
+    def ask(v):
+        full = v if v.dim() == 2 else v[None].expand(12, -1)
+        taken.extend(call(direct, full) for call in calls)
+        return v + 1.0
+    with FakeTensorMode(allow_non_fake_inputs=True) as mode:
+        ask(mode.from_tensor(t))
+        ask(t)
+    with Passes():
+        ask(t)
+        general = [_plain(call(lambda name, *args: PUBLIC[name](*args), t)) for call in calls]      # the general path serves them
+    assert all(torch.equal(a, b) for got, y in zip(general, expect) for a, b in zip(got, y))
+    torch.func.vmap(ask)(t)
+    torch.func.grad(lambda v: ask(v).sum())(t)
+    torch.func.jvp(ask, (t,), (torch.ones_like(t),))
+    torch.func.functionalize(ask)(t)
+    torch.jit.trace(ask, (t,), check_trace=False)
+    assert len(taken) == len(calls) * 8 and all(y is None for y in taken), [y is None for y in taken]
+    for call, y in zip(calls, expect):                            # and nothing of it is left behind
+        assert all(torch.equal(a, b) for a, b in zip(_plain(call(direct, t)), y))
