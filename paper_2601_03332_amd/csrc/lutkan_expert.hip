@@ -237,14 +237,14 @@ SortPlan plan_sort(int64_t choices, int experts) {
 int launch_sort(const SortArgs &a, const SortPlan &p, const char *who, hipStream_t s) {
   static LdsCap caps[3];
   const size_t counts = (size_t)p.waves * p.bins * sizeof(int), lds = counts + ((size_t)p.bins * (p.groups > 1 ? 2 : 1) + kSortWaves) * sizeof(int);
-  lutkan::plan_note("expert_sort groups=%d waves=%d; ", p.groups, p.waves);
+  const bool more = lds > 64 * 1024;                              // (below that no kernel's cap has to be raised)
   if (p.groups == 1) {
-    if (int rc = raise_lds_cap(lutkan_expert_sort_kernel<false>, &caps[0], who)) return rc;
+    if (int rc = more ? raise_lds_cap(lutkan_expert_sort_kernel<false>, &caps[0], who) : LUTKAN_OK) return rc;
     hipLaunchKernelGGL(lutkan_expert_sort_kernel<false>, dim3(1), dim3(64 * p.waves), lds, s, a);
     return check_launch(who);
   }
-  if (int rc = raise_lds_cap(lutkan_expert_count_kernel, &caps[1], who)) return rc;
-  if (int rc = raise_lds_cap(lutkan_expert_sort_kernel<true>, &caps[2], who)) return rc;
+  if (int rc = more ? raise_lds_cap(lutkan_expert_count_kernel, &caps[1], who) : LUTKAN_OK) return rc;
+  if (int rc = more ? raise_lds_cap(lutkan_expert_sort_kernel<true>, &caps[2], who) : LUTKAN_OK) return rc;
   hipLaunchKernelGGL(lutkan_expert_count_kernel, dim3(p.groups), dim3(64 * p.waves), counts, s, a);
   if (int rc = check_launch(who)) return rc;
   hipLaunchKernelGGL(lutkan_expert_sort_kernel<true>, dim3(p.groups), dim3(64 * p.waves), lds, s, a);
@@ -517,7 +517,6 @@ extern "C" int lutkan_expert_sort(const lutkan_expert_sort_args *p, void *hip_st
   a.expert = p->expert; a.rows = p->rows; a.places = p->places; a.group_sizes = p->group_sizes; a.counts = static_cast<int32_t *>(p->workspace);
   a.stride = p->expert_stride; a.choices = (int32_t)(p->tokens * p->top); a.top = p->top; a.experts = p->experts; a.expert_bytes = (int8_t)p->expert_bytes;
   a.bins = plan.bins; a.segment = plan.segment;
-  lutkan::plan_clear();
   if (plan.one_pass) return launch_sort(a, plan, who, s);
   int32_t *order = a.counts + plan.count_words, *sorted = order + a.choices;
   a.rows = a.places = a.group_sizes = nullptr;
