@@ -107,7 +107,8 @@ def main():
             end.record()
             torch.cuda.synchronize()
             off = float((y.float() - ref).norm() / ref.norm())
-            print(f"{tokens:6d} tokens, {block.codes:>4s}: {begin.elapsed_time(end) / 20 * 1000:9.1f} us a pass, output {off:.3f} from the unquantised block's", flush=True)
+            which = f", {block.codes:>4s}" if len(blocks) > 1 else ""
+            print(f"{tokens:6d} tokens{which}: {begin.elapsed_time(end) / 20 * 1000:9.1f} us a pass, output {off:.3f} from the unquantised block's", flush=True)
 
 
 if __name__ == "__main__":
