@@ -511,7 +511,7 @@ int lutkan_expert_sort(const lutkan_expert_sort_args *args, void *hip_stream);
  * [0, y_rows) adds nothing, whatever its weight is; a token without a place is zeros.  weights null: 1.  out and y must
  * not overlap.  With top = 1 and places = the rows of lutkan_expert_sort
  * it brings the tokens into the experts' order; the gradient of that is the same call without weights on the places.
- * Errors: EINVAL, ESHAPE (strides, rows), EUNSUPPORTED (strides, counts), EHIP. */
+ * Errors: EINVAL, ESHAPE (strides, rows), EUNSUPPORTED (strides or counts beyond 2^31 - 1, top or width beyond 2^30), EHIP. */
 typedef struct {
   const void *y;                            /* device [y_rows][width] of y_type */
   const void *places;                       /* device [tokens][top], contiguous, whole numbers of places_bytes (4 or 8) */

@@ -480,14 +480,14 @@ void with_types(int first, int second, const F &f) {
   }
 }
 
-constexpr int kMostWidth = 1 << 30;                               // (columns are counted in 32 bits, past a row's end too)
+constexpr int kMostCounted = 1 << 30;                             // (columns, and a token's choices, are counted in 32 bits, past their end too)
 
 bool is_whole(int bytes) { return bytes == 4 || bytes == 8; }
 
 // What both directions check: the counts and the tokens' rows.
 int check_tokens(const char *who, int64_t tokens, int32_t top, int32_t width, int64_t y_rows) {
   if (tokens < 0 || top < 1 || width < 1 || y_rows < 0) return fail(LUTKAN_EINVAL, "%s: %lld tokens, %d each, width %d, %lld rows", who, (long long)tokens, top, width, (long long)y_rows);
-  if (width > kMostWidth) return fail(LUTKAN_EUNSUPPORTED, "%s: width %d, at most %d", who, width, kMostWidth);
+  if (width > kMostCounted || top > kMostCounted) return fail(LUTKAN_EUNSUPPORTED, "%s: width %d, %d choices a token, at most %d", who, width, top, kMostCounted);
   if (tokens > INT32_MAX || y_rows > INT32_MAX) return fail(LUTKAN_EUNSUPPORTED, "%s: at most 2^31 - 1 tokens and rows", who);
   return LUTKAN_OK;
 }

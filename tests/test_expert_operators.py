@@ -528,3 +528,16 @@ def test_native_calls_leave_deferred_and_traced_operators_to_the_general_path():
     assert len(taken) == len(calls) * 8 and all(y is None for y in taken), [y is None for y in taken]
     for call, y in zip(calls, expect):                            # and nothing of it is left behind
         assert all(torch.equal(a, b) for a, b in zip(_plain(call(direct, t)), y))
+
+
+# ---------------------------------------------------------------- ends of ranges
+def test_more_choices_a_token_than_the_loops_count_are_refused():
+    """A token's choices are looked through 64 (the rows of y: four) at a time, counted in 32 bits: the count behind the last ones has to fit them."""
+    import ctypes as C
+    lib = lk.load_library()
+    for top in ((1 << 30) + 1, (1 << 31) - 64, (1 << 31) - 63, (1 << 31) - 1):
+        a = binding._ExpertCombineArgs(4096, 4096, 4096, 4096, 6, 8, 8, 1, top, 8, 0, 0, 0, 4)
+        _refused(-5, lib.lutkan_expert_combine(C.byref(a), None))
+        a = binding._ExpertCombineBackwardArgs(4096, 4096, 4096, 4096, 4096, 4096, 4096, 6, 8, 8, 8, 1, top, 8, 0, 0, 0, 4, 4)
+        _refused(-5, lib.lutkan_expert_combine_backward(C.byref(a), None))
+    assert lib.lutkan_expert_combine(C.byref(binding._ExpertCombineArgs(None, None, None, None, 6, 8, 8, 0, 1 << 30, 8, 0, 0, 0, 4)), None) == 0
