@@ -965,7 +965,8 @@ def lutkan_grouped_matmul_fp8(x, x_scales, weight, weight_scales, group_sizes, r
 # ---------------------------------------------------------------- 8-bit integers (see lutkan.h)
 def lutkan_rmsnorm_int8(x, weight, residual=None, eps: float = 1e-6, residual_out=None):
     """lutkan_rmsnorm_fp8 with integer codes and one scale a row: returns (codes, scales, residual_out), int8 [rows, width], float32 [rows], and
-    x + residual in the residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself."""
+    x + residual in the residual's dtype (None without one).  residual_out: where that goes; it may be the residual itself.  Codes and scales, which
+    are used together, may share one allocation (a program that saves them clones them first)."""
     if residual_out is None:
         out = (_native or _native_calls()).rmsnorm_int8(x, weight, residual, eps)
         if out is not None:
@@ -999,7 +1000,7 @@ def lutkan_rmsnorm_int8(x, weight, residual=None, eps: float = 1e-6, residual_ou
 
 def lutkan_quantise_int8(x):
     """(codes, scales) of a weight [n, k], of one weight per expert [experts, n, k], or of tokens [rows, k]: int8 of x's shape and a float32 scale
-    for each row of it ([n], [experts, n], [rows]), for the products below."""
+    for each row of it ([n], [experts, n], [rows]), for the products below; each in an allocation of its own, as a program saves them."""
     out = (_native or _native_calls()).quantise_int8(x)
     if out is not None:
         return out

@@ -314,15 +314,9 @@ PyObject *quantise(PyObject *, PyObject *const *args, Py_ssize_t n) {
     at::Tensor codes, scales;
     const bool ok = on_device(*w, [&](void *stream) {
       const auto options = w->options().requires_grad(false);
-      if constexpr (INT8) {
-        const int64_t scales_at = (w->numel() + 255) / 256 * 256;
-        const at::Tensor held = at::empty({scales_at + (several ? w->size(0) : 1) * rows * 4}, options.dtype(at::kByte));
-        codes = tensor_in(held, 0, at::kChar, w->sizes());
-        scales = tensor_in(held, scales_at, at::kFloat, w->sizes().slice(0, w->dim() - 1));
-      } else {
-        codes = at::empty(w->sizes(), options.dtype(at::kFloat8_e4m3fn));
-        scales = several ? at::empty({w->size(0), blocks(rows), blocks(k)}, options.dtype(at::kFloat)) : at::empty({blocks(rows), blocks(k)}, options.dtype(at::kFloat));
-      }
+      codes = at::empty(w->sizes(), options.dtype(INT8 ? at::kChar : at::kFloat8_e4m3fn));          // (each in a storage of its own: weights are saved)
+      if (INT8) scales = at::empty(w->sizes().slice(0, w->dim() - 1), options.dtype(at::kFloat));
+      else scales = several ? at::empty({w->size(0), blocks(rows), blocks(k)}, options.dtype(at::kFloat)) : at::empty({blocks(rows), blocks(k)}, options.dtype(at::kFloat));
       return (INT8 ? g.quantise_int8 : g.quantise)(w->const_data_ptr(), type_of(*w), several ? w->size(0) : 1, (int32_t)rows, (int32_t)k, row_stride(*w), several ? w->stride(0) : 0,
                         codes.mutable_data_ptr(), scales.mutable_data_ptr<float>(), stream);
     });

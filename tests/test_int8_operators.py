@@ -476,3 +476,22 @@ def test_the_binding_refuses_operands_that_do_not_fit():
     _raises("residual_out must", lk.lutkan_rmsnorm_int8, v, torch.ones(130, device=DEV), residual=v, residual_out=v.half())
     _raises("\\[-5\\]", lk.lutkan_rmsnorm_int8, torch.zeros(1, 40000, device=DEV), torch.ones(40000, device=DEV))
     _raises("\\[-5\\]", lk.lutkan_quantise_int8, torch.zeros(1, 131072, device=DEV))
+
+
+# ---------------------------------------------------------------- converted weights, kept
+@gpu
+@pytest.mark.parametrize("general", [False, True], ids=["native", "general"])
+@pytest.mark.parametrize("shape", [(300, 200), (8, 30, 70), (3, 40000)], ids=str)
+def test_converted_weights_are_saved_and_loaded(shape, general, monkeypatch):
+    """Codes and scales lie in storages of their own: formats that store whole storages, each of one type, take both."""
+    import io
+    if general:
+        monkeypatch.setattr(binding, "_native", binding._GeneralPath)
+    codes, scales = lk.lutkan_quantise_int8(torch.randn(shape, generator=torch.Generator().manual_seed(1)).to(DEV))
+    held = [(t.untyped_storage().nbytes(), t.storage_offset()) for t in (codes, scales)]
+    assert held == [(codes.numel(), 0), (4 * scales.numel(), 0)]
+    file = io.BytesIO()
+    torch.save({"codes": codes, "scales": scales}, file)
+    file.seek(0)
+    loaded = torch.load(file, weights_only=True)
+    assert torch.equal(loaded["codes"], codes) and torch.equal(loaded["scales"], scales)
