@@ -388,14 +388,16 @@ PyObject *expert_sort(PyObject *, PyObject *const *args, Py_ssize_t n) {
     at::Tensor rows, places, sizes;
     const bool ok = on_device(*e, [&](void *stream) {
       const size_t needed = g.sort_workspace_bytes(tokens, (int32_t)top, (int32_t)experts);
-      const int64_t each = (tokens * top * 4 + 255) / 256 * 256, sizes_at = 2 * each, workspace_at = sizes_at + (experts * 4 + 255) / 256 * 256;
-      const at::Tensor held = at::empty({workspace_at + (int64_t)needed}, e->options().requires_grad(false).dtype(at::kByte));      // one allocation for all
+      const int64_t each = (tokens * top * 4 + 255) / 256 * 256, sizes_at = 2 * each;
+      const auto bytes = e->options().requires_grad(false).dtype(at::kByte);
+      const at::Tensor held = at::empty({sizes_at + experts * 4}, bytes);             // one allocation for the outputs
+      const at::Tensor workspace = needed ? at::empty({(int64_t)needed}, bytes) : at::Tensor();         // (free again behind the call)
       rows = tensor_in(held, 0, at::kInt, {tokens * top});
       places = tensor_in(held, each, at::kInt, {tokens, top});
       sizes = tensor_in(held, sizes_at, at::kInt, {experts});
       lutkan_expert_sort_args a{};
       a.expert = e->const_data_ptr(); a.rows = rows.mutable_data_ptr<int32_t>(); a.places = places.mutable_data_ptr<int32_t>(); a.group_sizes = sizes.mutable_data_ptr<int32_t>();
-      a.workspace = needed ? static_cast<char *>(held.mutable_data_ptr()) + workspace_at : nullptr; a.workspace_bytes = needed;
+      a.workspace = needed ? workspace.mutable_data_ptr() : nullptr; a.workspace_bytes = needed;
       a.expert_stride = row_stride(*e); a.tokens = tokens; a.top = (int32_t)top; a.experts = (int32_t)experts; a.expert_bytes = (int32_t)e->element_size();
       return g.sort(&a, stream);
     });

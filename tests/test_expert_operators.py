@@ -541,3 +541,59 @@ def test_more_choices_a_token_than_the_loops_count_are_refused():
         a = binding._ExpertCombineBackwardArgs(4096, 4096, 4096, 4096, 4096, 4096, 4096, 6, 8, 8, 8, 1, top, 8, 0, 0, 0, 4, 4)
         _refused(-5, lib.lutkan_expert_combine_backward(C.byref(a), None))
     assert lib.lutkan_expert_combine(C.byref(binding._ExpertCombineArgs(None, None, None, None, 6, 8, 8, 0, 1 << 30, 8, 0, 0, 0, 4)), None) == 0
+
+
+# ---------------------------------------------------------------- the sort's forms, and what its outputs hold on to
+def sort_form(tokens, top, experts):
+    """(several work-groups, two passes), from the workspace: counts of several work-groups, the two orders of two passes."""
+    need = lk.load_library().lutkan_expert_sort_workspace_bytes(tokens, top, experts)
+    orders = 8 * tokens * top if experts > 2048 else 0
+    assert need >= orders
+    return need > orders, experts > 2048
+
+
+def test_the_sorted_shapes_reach_every_form_of_the_sort():
+    forms = {shape: sort_form(*shape) for shape in SORTS}
+    assert set(forms.values()) == {(a, b) for a in (False, True) for b in (False, True)}
+    assert all(several == (shape[0] * shape[1] > 4096) for shape, (several, _) in forms.items())
+
+
+@gpu
+@pytest.mark.parametrize("general", [False, True], ids=["native", "general"])
+@pytest.mark.parametrize("shape", [(1, 2, 8), (2048, 2, 64), (16384, 8, 64), (3000, 1, 4096), (40000, 2, 70001)], ids=str)
+def test_a_sort_keeps_its_outputs_alone(shape, general, monkeypatch):
+    """The workspace is free again once the call has returned: a program that keeps places and rows for its backward pass keeps no more than these."""
+    if general:
+        monkeypatch.setattr(binding, "_native", binding._GeneralPath)
+    tokens, top, experts = shape
+    e = choices(4, tokens, top, experts, "dropped")
+    got = lk.lutkan_expert_sort(e.to(DEV), experts)
+    held = sum({t.untyped_storage().data_ptr(): t.untyped_storage().nbytes() for t in got}.values())
+    assert held <= sum(t.numel() * 4 + 255 for t in got)
+    again = [lk.lutkan_expert_sort(e.to(DEV), experts) for _ in range(3)] + [torch.full((3 * tokens * top + 70001,), 9, dtype=torch.int32, device=DEV)]      # (in the same memory)
+    for g, a, r in zip(got, again[0], sort_reference(e, experts)):
+        assert torch.equal(g.cpu(), r) and torch.equal(a.cpu(), r)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(9000, 2, 64), (3000, 1, 4096), (9000, 2, 4096)], ids=str)
+def test_sorts_in_two_replayed_graphs(shape):
+    """Two sorts a graph, two graphs of one pool of memory, replayed in turn with eager calls between them."""
+    tokens, top, experts = shape
+    given = [choices(k, tokens, top, experts, "dropped").to(DEV) for k in range(2)]
+    for e in given:
+        lk.lutkan_expert_sort(e, experts)
+    torch.cuda.synchronize()
+    graphs, outputs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for k, graph in enumerate(graphs):
+        with torch.cuda.graph(graph, pool=graphs[0].pool() if k else None):
+            outputs.append([lk.lutkan_expert_sort(e, experts) for e in given])
+    for k in range(4):
+        for graph, out in zip(graphs, outputs):
+            for i, e in enumerate(given):
+                e.copy_(choices(10 * k + i, tokens, top, experts, "any" if k == 1 else "dropped"))
+            graph.replay()
+            torch.cuda.synchronize()
+            for e, sorted_ in zip(given, out):
+                eager = lk.lutkan_expert_sort(e, experts)
+                assert all(torch.equal(a, b) and torch.equal(a.cpu(), r) for a, b, r in zip(sorted_, eager, sort_reference(e.cpu(), experts)))
