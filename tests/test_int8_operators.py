@@ -495,3 +495,46 @@ def test_converted_weights_are_saved_and_loaded(shape, general, monkeypatch):
     file.seek(0)
     loaded = torch.load(file, weights_only=True)
     assert torch.equal(loaded["codes"], codes) and torch.equal(loaded["scales"], scales)
+
+
+# ---------------------------------------------------------------- the norm, by the depth of its sums
+SCALE_DEPTH = 33 * U
+"""A lane adds at most 32 squares, one rounding each; six exchanges in a wave and at most 15 additions of the waves' sums follow, 53.  The mean has two more, and the root halves
+them all: 27.5.  The root and its reciprocal, two products and the scale's quotient are one each: 32.5."""
+CODE_DEPTH = 6.1 * U
+"""The root cancels in y / scale: two products each in y and in the largest, the scale's quotient and the code's."""
+
+
+def assert_norm_by_depth(codes, scales, y):
+    scale = y.abs().amax(1) / 127
+    assert bool(((scales.double() - scale).abs() <= SCALE_DEPTH * scale).all()), float((scales.double() / scale - 1).abs().max()) / U
+    quotient = y / scale[:, None]
+    off = (codes.double() - quotient).abs() - 0.5
+    assert bool((off <= CODE_DEPTH * quotient.abs()).all()), float((off / quotient.abs()).max()) / U
+
+
+@gpu
+@pytest.mark.parametrize("rows", [60, 1030, 2100])
+@pytest.mark.parametrize("width", [40, 511, 513, 1000, 1537, 2048, 3000, 4096, 5001, 8192, 16400, 32768])
+def test_norm_where_one_column_decides(rows, width):
+    """In each of the first rows one column, around the ends of lanes' columns, waves and the row, is 1000 times the others: a norm that misses it, or takes it twice, is far off.  The other
+    rows are of equal size throughout: a column there is 1 / (2 width) of the scale, seven times the bound at the widest."""
+    if rows * width > 20_000_000:
+        rows = 1030
+    gen = torch.Generator().manual_seed(width)
+    x = torch.randn(rows, width, generator=gen).to(DEV)
+    weight = (1 + 0.3 * torch.randn(width, generator=gen)).to(DEV)
+    columns = sorted({c + d for c in (0, 8, 512, 1024, 1536, 2048, 4096, 8192, 12288, 16384, 24576, width // 8 * 8, width) for d in (-8, -1, 0, 1, 7)} & set(range(width)))
+    for i in range(min(len(columns), rows)):
+        x[i, columns[i]] = 1000.0 * (-1) ** i
+    for power, eps in ((0, 1e-5), (70, 0.0), (-70, 0.0)):          # (squares in fp32's range, and beyond it on both sides)
+        print(f"case norm depth {rows} {width} {power}", flush=True)
+        h = x * 2.0 ** power
+        y = h.double() / torch.sqrt(h.double().square().mean(1, keepdim=True) + eps) * weight.double()
+        assert_norm_by_depth(*lk.lutkan_rmsnorm_int8(h, weight, eps=eps)[:2], y)
+    half, residual = x.bfloat16(), (2 * torch.randn(rows, width, generator=gen)).half().to(DEV)
+    h = half.float() + residual.float()
+    y = h.double() / torch.sqrt(h.double().square().mean(1, keepdim=True) + 1e-5) * weight.bfloat16().double()
+    codes, scales, out = lk.lutkan_rmsnorm_int8(half, weight.bfloat16(), residual=residual, eps=1e-5)
+    assert_norm_by_depth(codes, scales, y)
+    assert torch.equal(out, h.half())
