@@ -597,3 +597,53 @@ def test_sorts_in_two_replayed_graphs(shape):
             for e, sorted_ in zip(given, out):
                 eager = lk.lutkan_expert_sort(e, experts)
                 assert all(torch.equal(a, b) and torch.equal(a.cpu(), r) for a, b, r in zip(sorted_, eager, sort_reference(e.cpu(), experts)))
+
+
+# ---------------------------------------------------------------- the gradients, by the depth of their sums
+def gradient_depth(width):
+    """Roundings that a product of a weight's gradient passes through: eight fused additions for each of a lane's pieces of eight columns (up to 16 waves share a row),
+    six exchanges in a wave, the waves' sums."""
+    waves = min(-(-width // 512), 16)
+    return 8 * -(-width // (512 * waves)) + 6 + waves
+
+
+DEPTHS = [7, 300, 511, 513, 1025, 4103, 8191, 8192, 8193, 9001, 16385, 20007]
+
+
+@gpu
+@pytest.mark.parametrize("types", [(torch.float32, torch.float32), (torch.bfloat16, torch.float32), (torch.float32, torch.float16), (torch.float16, torch.bfloat16)], ids=str)
+@pytest.mark.parametrize("width", DEPTHS)
+def test_gradients_of_the_weights_by_the_depth_of_their_sums(width, types):
+    """The bound is well below what one column of average size adds: 46 u of A at most, where a column holds A / width."""
+    y_type, g_type = types
+    tokens, top, experts = 12, 5, 7
+    print(f"case depth {width} {types}", flush=True)
+    rows, places, y, weights, grad = joined(width, tokens, top, width, experts, "dropped", y_type, torch.float32, g_type)
+    gy, gw, A = gradient_reference(grad, y, places, weights)
+    got_y, got_w = lk.lutkan_expert_combine_backward(grad.to(DEV), y.to(DEV), rows.to(DEV), places.to(DEV), weights.to(DEV))
+    near(got_w, gw, gradient_depth(width) * U * 1.01 * A, "grad_weights")
+    near(got_y, gy, U * np.abs(gy), "grad_y")
+
+
+@gpu
+@pytest.mark.parametrize("types", [(a, b) for a in FLOATS for b in FLOATS], ids=str)
+@pytest.mark.parametrize("width", DEPTHS)
+def test_gradients_of_the_weights_where_one_column_decides(width, types):
+    """Each token's gradient has one column that is not zero, at the ends of the lanes' pieces, of the waves' and the work-group's columns and of the row: small whole
+    numbers, so that the sums are exact and a column that is left out, or taken twice, shows."""
+    y_type, g_type = types
+    columns = sorted({c + d for c in (0, 8, 512, 1024, 4096, 8192, 16384, width // 8 * 8, width) for d in (-8, -1, 0, 1, 7)} & set(range(width)))
+    tokens, top = len(columns), 5
+    print(f"case column {width} {types}", flush=True)
+    gen = torch.Generator().manual_seed(width)
+    rows, places, _ = sort_reference(choices(width, tokens, top, 6, "any"), 6)
+    y = torch.randint(1, 9, (tokens * top, width), generator=gen).to(y_type)
+    weights = torch.exp2(torch.randint(-3, 4, (tokens, top), generator=gen).float())
+    grad, at = torch.zeros(tokens, width, dtype=g_type), torch.tensor(columns)
+    value = torch.randint(1, 9, (tokens,), generator=gen)
+    grad[torch.arange(tokens), at] = value.to(g_type)
+    got_y, got_w = lk.lutkan_expert_combine_backward(grad.to(DEV), y.to(DEV), rows.to(DEV), places.to(DEV), weights.to(DEV))
+    assert torch.equal(got_w.cpu(), value[:, None].float() * y.float()[places.long(), at[:, None]])
+    expected = torch.zeros(y.shape)
+    expected[places.long()] = weights[..., None] * grad.float()[:, None, :]
+    assert torch.equal(got_y.cpu().float(), expected)
