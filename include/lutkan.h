@@ -74,7 +74,8 @@ const char *lutkan_version(void);
  * np=16 split=1 pipe=3; " (base_product cuts the base rows into pieces in a launch of its own) or, for a B-spline layer on the
  * matrix cores, "bspline_matrix np=1 split=2 slots=8; sum; " (slots: up to 8, 12 or 16 coefficient rows per input; model_forward: the clauses of all its layers), or, for a product in 8 bits,
  * "fp8_direct rows=16 columns=16 waves=8; " (a tile straight from memory, waves along the inputs) or "fp8_tiled rows=128 columns=128
- * teams=2 async; " (tiles through LDS; teams of waves along the inputs, copies without registers).  Thread-local, overwritten by the next forward call, never null. */
+ * teams=2 async; " (tiles through LDS; teams of waves along the inputs, copies without registers), "int8_" for integer codes.  Thread-local, overwritten by the next
+ * forward call or product, never null; all other calls (statistics, norms, conversions, a mixture's sort and joining) leave it as it was. */
 const char *lutkan_last_plan(void);
 
 /* ------------------------------------------------------------------------------------------------
@@ -471,7 +472,8 @@ int lutkan_grouped_matmul_fp8(const lutkan_matmul_fp8_args *args, void *hip_stre
 int lutkan_rmsnorm_int8(const lutkan_rmsnorm_fp8_args *args, void *hip_stream);
 
 /* Rows [matrices][n][k] of a lutkan_type (a weight's outputs, or tokens) to codes [matrices][n][k] and scales [matrices][n], both
- * contiguous.  k is at most LUTKAN_INT8_MAX_INPUTS.  Errors: EINVAL, ESHAPE (negative strides), EUNSUPPORTED, EHIP. */
+ * contiguous.  k is at most LUTKAN_INT8_MAX_INPUTS.  One launch where the matrices follow each other at the distance of their rows or have a single row, else one for
+ * each matrix.  Errors: EINVAL, ESHAPE (negative strides), EUNSUPPORTED, EHIP. */
 int lutkan_quantise_int8(const void *rows, int32_t type, int64_t matrices, int32_t n, int32_t k, int64_t stride, int64_t matrix_stride,
                          void *codes, float *scales, void *hip_stream);
 
@@ -529,7 +531,8 @@ int lutkan_expert_combine(const lutkan_expert_combine_args *args, void *hip_stre
  * rows of grad_y that no place leads to are zeros, and so is grad_weights of a choice without a place.  Several places must not be equal.
  * Without weights, y is not read and grad_weights not written: both null.  The outputs
  * must not overlap the inputs.  y and grad_y have one type, weights and grad_weights too.
- * The order of the sums depends on the sizes, not on the run: equal calls give equal bits.  Errors as lutkan_expert_combine. */
+ * The order of the sums depends on the sizes, not on the run: equal calls give equal bits.  Errors as lutkan_expert_combine; it is one launch, with 64 threads to
+ * a token for each 512 columns, at most 1024: calls of 2^32 threads (2^26 tokens up to 512 columns, 2^22 from 7681 on) are EUNSUPPORTED. */
 typedef struct {
   const void *grad;                         /* device [tokens][width] of grad_type */
   const void *y;                            /* device [y_rows][width] of y_type; null without weights */

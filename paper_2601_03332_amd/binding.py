@@ -1172,7 +1172,8 @@ def lutkan_expert_combine(y, places, weights=None, out=None, dtype=None):
 def lutkan_expert_combine_backward(grad, y, rows, places, weights=None):
     """The gradients of lutkan_expert_combine(y, places, weights) for the gradient grad [tokens, width] of its output: (grad_y [rows, width] in y's
     dtype, grad_weights [tokens, top] in the weights'; None without weights).  rows and places are of one lutkan_expert_sort; rows of grad_y that
-    no place leads to are zeros.  The operators take no part in torch's autograd: a program calls this from its own backward pass."""
+    no place leads to are zeros.  The operators take no part in torch's autograd: a program calls this from its own backward pass, around experts
+    that have one (a compiled table layer has none)."""
     out = (_native or _native_calls()).expert_combine_backward(grad, y, rows, places, weights)
     if out is not None:
         return out

@@ -26,7 +26,7 @@ static_assert(sizeof(SortArgs) <= 112, "launch");
 
 constexpr int kSortWaves = 16;
 // Chunks of 64 choices whose experts a wave holds; their loop is unrolled, and a longer code costs more to fetch than it saves (with 16 of them 524288 choices take
-// 16.2 us for 13.3, one token 3.9 for 3.3).
+// 16.2 us for 11.9, one token 3.9 for 3.3).
 constexpr int kSortHeld = 4;
 // Choices of one work-group's launch: 4080 of 64 experts take 7.8 us and 4800 10.2, two launches of several work-groups 8.4 for these.
 constexpr int kSortSingle = 64 * kSortHeld * kSortWaves;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_count_kernel(co
 // A counting sort: the place of a choice is the number of choices of lower bins, of its bin in work-groups and waves before its own, and before it
 // in its wave.  The last comes from ballots over the bits of the bin, so that equal bins keep their order and no atomic decides it (the atomics
 // here count).  Bound by latencies: launches, a chain of loads, counts and scans: one token's 2 choices 2.7 us (a launch alone 2.4), 524288 choices of 64 experts
-// 3.6 + 9.8, where their bytes take 1.6.
+// 3.6 + 9.8, where their bytes take 1.6.  Two passes: of 4096 experts 120 us, where 2048 take 41.
 template <bool SEVERAL>
 __global__ __launch_bounds__(64 * kSortWaves) void lutkan_expert_sort_kernel(const SortArgs a) {
   extern __shared__ int s_count[];                                // [waves][bins], then the bins' totals, later first places, the waves' sums, the bins' counts before
@@ -220,7 +220,7 @@ SortPlan plan_sort(int64_t choices, int experts) {
     p.groups = 1;
   } else {
     // More work-groups are shorter, and each reads the counts of all: 524288 choices of 256 experts take 21.2 us with 81 of them, 16.9 with 160; of 64
-    // experts 17.6, 13.4 and 12.8 with 112, 160 and 256.
+    // experts 17.5, 13.3 and 12.5 with 112, 160 and 256.
     const double best = std::sqrt(800.0 * (double)chunks / std::min(experts + 1, 1 << kSortDigit));
     const int64_t most = (int64_t)kSortWaves * std::max(1, (int)std::min(best, 256.0)), of_wave = (chunks + most - 1) / most;
     p.waves = kSortWaves;
@@ -330,7 +330,7 @@ struct Choices {
 constexpr int kJoined = 4;                                       // rows that are read before the first is used
 
 // A wave sums 512 columns of one token, eight a lane.  ONCE: several rows a token, which no other token has.
-// Bound by memory: 16384 tokens of four rows of 2048 (bf16) 60 - 67 us, 5.0 - 5.6 TB/s; 16 tokens of two of 1024 (fp32) 3.0.
+// Bound by memory: 16384 tokens of four rows of 2048 (bf16) 60 - 67 us, 5.0 - 5.6 TB/s (an addition of two tensors, two reads to a write: 6.0); 16 tokens of two of 1024 (fp32) 3.0.
 template <int Y, int O, bool ONCE>
 __global__ __launch_bounds__(256) void lutkan_expert_combine_kernel(const CombineArgs a) {
   const int lane = threadIdx.x & 63, pieces = (a.width + 511) / 512;

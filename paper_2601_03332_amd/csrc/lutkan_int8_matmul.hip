@@ -552,7 +552,7 @@ int launch_tiles(const ProductArgs &a, int64_t row_tiles, bool async, const char
 
 // What a launch takes beyond an empty one (2.4 us in a replayed graph), in us, for the kernels' choice.  The constants were fitted to 650 drawn calls of 1 to
 // 32768 rows, 16 to 8192 inputs and 2 to 8192 outputs, a third of them with rows at odd addresses, half by expert, each timed with every kernel; on 260 others the
-// kernel that is taken was within 2 % of the quickest in 220, 1.02 times it in the geometric mean, 1.5 at worst (few steps of many tiles).  Tried beside these, and
+// kernel that is taken was within 2 % of the quickest in 220, 1.02 times it in the geometric mean, 1.33 at worst (of all 910: 1.46, few steps of many tiles).  Tried beside these, and
 // not worth their place: direct tiles of 32 x 32, four teams on 64 x 64, two on 128 x 128 (each is the quickest of 1 - 4 % of the calls, by little).
 //   direct   what its work-groups read, each its own, over the whole GPU, and their number
 //   tiled    rounds of as many tiles as fit the compute units, a tile's steps of 128 k: `one` where there is one to a compute unit, `all` where

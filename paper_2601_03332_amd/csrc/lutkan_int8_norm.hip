@@ -67,7 +67,8 @@ __device__ __forceinline__ void read8_of(int type, const unsigned char *row, int
 // stays in a register as fp32; lane l of a row's lanes holds the eight columns 8 (l + lanes c), c < CH.
 // NORM: the codes do not depend on the norm, the scale does, so that one reduction gives the sum of squares and the largest |h weight|
 // together.  Where either leaves fp32's range the row is summed again with a power of 2 on h, and the norm applied before the product.
-// Bound by memory: 32768 rows of 1024 (bf16, residual bf16) 43 us replayed, 5.5 TB/s, where a copy of 1 GiB reaches 5.2.  One row of 1024: 3.0, of which a launch
+// Bound by memory: 32768 rows of 1024 (bf16, residual bf16), four bytes read to three written, 43 us replayed, 5.4 TB/s; a copy reaches 4.7 - 5.2, an addition of two
+// tensors (two read to one written) 6.0.  One row of 1024: 3.0, of which a launch
 // 2.4; 2400 rows of 200 (fp32, no norm) 3.2.
 template <int X, int R, int CH, bool NORM>
 __global__ __launch_bounds__(1024) void lutkan_int8_rows_kernel(const RowArgs a) {
